@@ -312,7 +312,8 @@ def _written(x, slots, codes, scale, ps):
     old = torch.where((first > 0)[:, None], scale, 0)
     new = torch.where((first < ps)[:, None], torch.maximum(want, old), scale)
     shrink = torch.where(new > 0, scale / new, 1).clamp(max=1)[:, :, None, None]
-    codes = torch.where((new != scale)[:, :, None, None], (codes.float() * shrink).round(), codes.float())
+    earlier = torch.arange(ps, device=y.device) < first[:, None]      # tokens that the page held before
+    codes = torch.where((new != scale)[:, :, None, None] & earlier[:, None, :, None], (codes.float() * shrink).round(), codes.float())
     codes = torch.cat([codes, codes[:1]])
     s = torch.cat([new, new[:1]])[page][..., None]
     codes[page, :, torch.where(real, slots % ps, 0).long()] = torch.where(s > 0, y / s, 0).round().clamp(-127, 127)
@@ -445,7 +446,8 @@ def _exact_write(case, s):
             top = np.abs(x[part]).max(axis=(0, 2))
             want = np.array([0.0 if t == 0 else 2.0 ** next(e for e in range(-160, 130) if 127 * 2.0 ** e >= t) for t in top])
             grown = np.maximum(want, scale[p] if at[0] > 0 else 0)
-            codes[p] = np.rint(codes[p] * np.where(grown > 0, np.minimum(scale[p] / np.where(grown > 0, grown, 1), 1), 1)[:, None, None])
+            shrink = np.where(grown > 0, scale[p] / np.where(grown > 0, grown, 1), 1)[:, None, None]
+            codes[p][:, :at[0]] = np.rint(codes[p][:, :at[0]] * shrink)
             codes[p][:, at] = np.rint(x[part] / np.where(grown > 0, grown, 1)[None, :, None]).transpose(1, 0, 2)
             scale[p] = grown
         got += [codes.astype(np.int8), scale]
