@@ -135,6 +135,7 @@ typedef struct {
 #define RTPRUNE_DEV_NONFINITE 1u
 #define RTPRUNE_DEV_TIMEOUT 2u
 #define RTPRUNE_DEV_BAD_OFFSETS 4u /* an image had N_i < 1 or N_i > max_tokens_per_image */
+#define RTPRUNE_DEV_NO_PAGES 8u    /* the free list or a table row was too short (rtprune_page_map only) */
 
 /* Fills *params with the paper's defaults: fixed r = 0.25, z = 0.2, alpha = 0.1, eps = 1,
  * iters = 100, identity f_normalize, r_max = 1, form AUTO, stop_at_fixed_point = 1, tol = 0,
@@ -319,6 +320,116 @@ rtprune_status_t rtprune_density(void *cuda_stream, const uint8_t *images, int32
 rtprune_status_t rtprune_test_density_expired(void *cuda_stream, const uint8_t *images, int32_t batch, int32_t height,
                                               int32_t width, int32_t patch, float tau, float *rho,
                                               uint32_t *image_counts, int32_t *edge_counts);
+
+/*
+ * From the packed output to the answer: the prefill of the kept tokens and the decode after it.  The pruned lengths are
+ * known on the device only (dynamic ratio), so the pages of a key/value cache are handed out there (rtprune_page_map),
+ * queries and keys are normed and rotated by the positions of the KEPT tokens (rtprune_qk_norm_rope), keys and values go
+ * into pages of 8-bit codes (rtprune_cache_write), and attention reads those pages (rtprune_cache_attend).  Requests are a
+ * ragged batch in the layout of rtprune_run's output: `offsets` is its out_offsets, rows behind offsets[batch] belong to no
+ * request.  These calls need no plan; they are asynchronous on the stream, allocate nothing, keep nothing between calls and may be captured.
+ *
+ * The cache: num_pages pages of page_size token slots; slot s is token s mod page_size of page s div page_size.  Token t of a
+ * request is in the page that entry t div page_size of its row of the block table names.  A page holds, for each kv head,
+ * page_size x head_dim codes for the keys and as many for the values, and one scale for each: a key's value is code * scale.
+ * Scales start at zero (all of k_scale, v_scale cleared once); codes need no start value.
+ */
+typedef struct {
+    int8_t *k, *v;            /* DEVICE [num_pages][kv_heads][page_size][head_dim] codes, 16-byte aligned */
+    float *k_scale, *v_scale; /* DEVICE [num_pages][kv_heads]                                             */
+    int64_t num_pages;        /* num_pages * page_size <= 2^31 - 1                                        */
+    int32_t page_size;        /* 16, 32, 64 or 128                                                        */
+    int32_t kv_heads;         /* at most 1024                                                             */
+    int32_t head_dim;         /* 64 or 128                                                                */
+} rtprune_cache_t;
+
+/*
+ * Block tables, slots and positions of a batch's new tokens.  Request i has context_lens[i] tokens in the pages of its
+ * table row already (0 without context_lens) and offsets[i+1] - offsets[i] new ones.  The pages that it needs beyond
+ * those it has come from the free list, in the order of the requests, from entry *free_head on.
+ *
+ *   offsets       DEVICE int32 [batch+1], non-decreasing from 0, at most total_rows; batch <= 16384
+ *   total_rows    rows of slot_map and positions: a capacity, known without the device's lengths
+ *   token_index   DEVICE int32 [total_rows] or NULL: rtprune_run's kept_idx.  A token's position is then
+ *                 position_base[i] + token_index[row], else position_base[i] + its number among the new tokens;
+ *   position_base DEVICE int32 [batch] or NULL (then context_lens)
+ *   free_pages    DEVICE int32 [n_free] page ids; free_head DEVICE int32 [1]
+ *   block_tables  DEVICE int32 [batch] rows, table_stride apart, of max_pages entries: those of new pages are written, all others kept
+ * Outputs, DEVICE int32: slot_map [total_rows] (-1 in rows of no request), positions [total_rows] (-1 there; may be NULL),
+ * seq_lens [batch] (cached and new tokens), state [2] = {*free_head + pages handed out, RTPRUNE_DEV_* bits}.
+ * `state` must not be `free_head`.  Where the free list or a table row is too short, the tokens
+ * without a page get slot -1 (their table entry -1) and RTPRUNE_DEV_NO_PAGES is set; a request whose lengths are outside the contract gets
+ * no pages, slots -1 and length 0, and RTPRUNE_DEV_BAD_OFFSETS is set.  One kernel.
+ */
+rtprune_status_t rtprune_page_map(void *cuda_stream, const int32_t *offsets, const int32_t *context_lens, int32_t batch,
+                                  int64_t total_rows, const int32_t *token_index, const int32_t *position_base,
+                                  const int32_t *free_pages, const int32_t *free_head, int32_t n_free, int32_t page_size,
+                                  int32_t *block_tables, int64_t table_stride, int32_t max_pages, int32_t *slot_map,
+                                  int32_t *positions, int32_t *seq_lens, int32_t *state);
+
+/*
+ * Norms of queries and keys and the rotation by position, for each head of each row: y = x w / sqrt(mean(x^2) + eps) over the
+ * head's elements (y = x where the weight is NULL), then pairs of the first rotary_dim elements turned by the angle
+ * positions[row] * inv_freq[p]: (y_a, y_b) -> (y_a cos - y_b sin, y_b cos + y_a sin).  Pair p is (p, p + rotary_dim/2), or
+ * (2p, 2p+1) with `interleaved`.  Sums and rotation in fp32, angles in 64 bits, one rounding at the end.  A row whose position
+ * is negative is left as it is in the outputs.
+ *
+ *   q, k          DEVICE [rows] rows of q_heads / kv_heads heads of head_dim, dtype; 16-byte aligned, row strides in elements, multiples of
+ *                 16 bytes (so that they may be parts of a fused projection's rows).  Either may have 0 heads.
+ *   q_out, k_out  DEVICE, likewise; may be q, k themselves with the same strides, and must not overlap them otherwise
+ *   weights       DEVICE [head_dim], dtype, 16-byte aligned, or NULL
+ *   inv_freq      DEVICE double [rotary_dim / 2], radians per position
+ * head_dim and rotary_dim multiples of 16, rotary_dim <= head_dim <= 256 (else RTPRUNE_ERR_UNSUPPORTED).  One kernel.
+ */
+rtprune_status_t rtprune_qk_norm_rope(void *cuda_stream, rtprune_dtype_t dtype, const void *q, int64_t q_stride, const void *k,
+                                      int64_t k_stride, int64_t rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                      const void *q_weight, const void *k_weight, float eps, const int32_t *positions,
+                                      const double *inv_freq, int32_t rotary_dim, int32_t interleaved, void *q_out,
+                                      int64_t q_out_stride, void *k_out, int64_t k_out_stride);
+
+/*
+ * Writes keys and values to their slots.  Tokens of one page are neighbouring rows with ascending, consecutive slots, as
+ * rtprune_page_map hands them out, and a page's new tokens follow those that it holds: of a page whose first new token is its
+ * token a, tokens 0 .. a-1 are earlier ones, the others are not read.  For each page that gets tokens and each head, separately for keys and values:
+ * s = the smallest power of two (at least 2^-126) with 127 s >= every |x| of the new tokens, 0 if they are all 0, and at least the old scale if
+ * the page has earlier tokens; where that grew, the earlier codes become rint(code * old / s); the new codes are rint(x / s).
+ * A block that gets a NaN or an infinity has scale NaN from then on, until its page is written from its first token again, and these tokens' codes are 0.
+ * A row with a slot outside the cache (-1) is passed over.  A page that gets rows of two separate runs in one call is not allowed: one run's
+ * scale is then lost (nothing is written outside the page).
+ *
+ *   k, v    DEVICE [rows] rows of kv_heads heads of head_dim, dtype; aligned and strided as in rtprune_qk_norm_rope
+ * One kernel.
+ */
+rtprune_status_t rtprune_cache_write(void *cuda_stream, rtprune_dtype_t dtype, const void *k, int64_t k_stride, const void *v,
+                                     int64_t v_stride, int64_t rows, const int32_t *slot_map, const rtprune_cache_t *cache);
+
+/*
+ * Attention of ragged queries over the cache.  Request i's n_i = offsets[i+1] - offsets[i] rows are the last n_i of its
+ * L_i = seq_lens[i] tokens, which are all in the cache: its row j sees tokens t <= L_i - n_i + j, or with causal = 0 all L_i.
+ *   s_t = scale * (q . k_t),   out = sum_t softmax(s)_t v_t,   lse = log sum_t exp(s_t)
+ * Query head h reads kv head h / (q_heads / kv_heads).  A row that sees nothing gives out = 0, lse = -inf.  A row that sees a block of
+ * scale NaN, or whose query is not finite, gives NaN, and so does a row of a request that sees an entry of its table outside the cache or whose
+ * seq_lens is outside 0 .. max_seq_len.  A request of more than max_q_len rows is passed over.  Values agree with those formulas in 64 bits to
+ * the rounding of bf16; the softmax and all sums are fp32.  What a row's result is does not depend on the call's timing.
+ *
+ *   q            DEVICE bf16 [rows] rows of q_heads heads of head_dim, 16-byte aligned, row stride in elements, a multiple of 8
+ *   offsets      DEVICE int32 [batch+1], seq_lens DEVICE int32 [batch]; batch <= 65535
+ *   max_q_len, max_seq_len  HOST upper bounds of n_i and L_i, max_seq_len <= max_pages * page_size; they choose the kernels and the
+ *                grid, not the result
+ *   block_tables DEVICE int32 [batch] rows, table_stride apart, of max_pages entries
+ *   out          DEVICE bf16 [rows][q_heads][head_dim], 16-byte aligned; lse DEVICE float [rows][q_heads], may be NULL.
+ *                Rows of no request are left as they are.
+ *   workspace    DEVICE, 256-byte aligned, of what rtprune_cache_attend_workspace says for the same sizes; its contents do not
+ *                matter and it serves one call at a time
+ * q_heads a multiple of kv_heads, at most 4096.
+ */
+rtprune_status_t rtprune_cache_attend_workspace(int32_t batch, int32_t max_q_len, int64_t max_seq_len, int32_t q_heads,
+                                                int32_t kv_heads, int32_t head_dim, size_t *workspace_bytes);
+rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *q, int64_t q_stride, int64_t rows, int32_t q_heads,
+                                      const int32_t *offsets, const int32_t *seq_lens, int32_t batch, int32_t max_q_len,
+                                      int64_t max_seq_len, const int32_t *block_tables, int64_t table_stride, int32_t max_pages,
+                                      const rtprune_cache_t *cache, float scale, int32_t causal, void *out, float *lse,
+                                      void *workspace, size_t workspace_bytes);
 
 /*
  * Test aid: makes the library's bounded device-side waits run out without any fault.  Launches one small

@@ -10,7 +10,7 @@ import ctypes
 import numpy as np
 import os
 from dataclasses import dataclass
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -20,7 +20,7 @@ STATS_STRIDE = 8
 BF16, FP32 = 0, 1
 SINKHORN_AUTO, SINKHORN_LOG, SINKHORN_SCALING, SINKHORN_EXACT = 0, 1, 2, 3
 SCHEDULE_AUTO, SCHEDULE_SEPARATE, SCHEDULE_FUSED = 0, 1, 2
-DEV_NONFINITE, DEV_TIMEOUT, DEV_BAD_OFFSETS = 1, 2, 4
+DEV_NONFINITE, DEV_TIMEOUT, DEV_BAD_OFFSETS, DEV_NO_PAGES = 1, 2, 4, 8
 
 STATUS_NAMES = {0: "RTPRUNE_OK", 1: "RTPRUNE_ERR_INVALID_ARG", 2: "RTPRUNE_ERR_UNSUPPORTED",
                 3: "RTPRUNE_ERR_WORKSPACE", 4: "RTPRUNE_ERR_CUDA", 5: "RTPRUNE_ERR_NONFINITE",
@@ -41,6 +41,13 @@ class CParams(ctypes.Structure):
                 ("eps", ctypes.c_float), ("iters", ctypes.c_int32), ("form", ctypes.c_int32),
                 ("stop_at_fixed_point", ctypes.c_int32), ("tol", ctypes.c_float),
                 ("criterion", ctypes.c_int32), ("schedule", ctypes.c_int32)]
+
+
+class CCache(ctypes.Structure):
+    """rtprune_cache_t."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("num_pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -78,6 +85,13 @@ def lib() -> ctypes.CDLL:
     L.rtprune_query_status.argtypes = [vp, vp, vp, ctypes.POINTER(ctypes.c_uint32)]
     L.rtprune_density.argtypes = [vp, vp, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp]
     L.rtprune_test_density_expired.argtypes = L.rtprune_density.argtypes
+    pc, f32 = ctypes.POINTER(CCache), ctypes.c_float
+    L.rtprune_page_map.argtypes = [vp, vp, vp, i32, i64, vp, vp, vp, vp, i32, i32, vp, i64, i32, vp, vp, vp, vp]
+    L.rtprune_qk_norm_rope.argtypes = [vp, i32, vp, i64, vp, i64, i64, i32, i32, i32, vp, vp, f32, vp, vp, i32, i32, vp, i64, vp,
+                                       i64]
+    L.rtprune_cache_write.argtypes = [vp, i32, vp, i64, vp, i64, i64, vp, pc]
+    L.rtprune_cache_attend_workspace.argtypes = [i32, i32, i64, i32, i32, i32, ctypes.POINTER(sz)]
+    L.rtprune_cache_attend.argtypes = [vp, vp, i64, i64, i32, vp, vp, i32, i32, i64, vp, i64, i32, pc, f32, i32, vp, vp, vp, sz]
     L.rtprune_profile_enable.argtypes = [vp, i32]
     L.rtprune_profile_read.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(ctypes.c_float),
                                        ctypes.POINTER(ctypes.c_char_p)]
@@ -347,6 +361,181 @@ def density(images: torch.Tensor, patch: int = 64, tau: float = 0.2, *, want_pat
         with torch.cuda.device(dev):
             _check(lib().rtprune_density(_stream_handle(stream), *args), "rtprune_density")
     return rho, counts, per_patch
+
+
+# ---- from the packed output to the answer: page tables, norms and rotation, the 8-bit cache, attention over it ---------
+
+class PagedCache(NamedTuple):
+    """Keys and values of cached tokens as 8-bit codes in pages, with a power-of-two scale per page and kv head (rtprune_cache_t).
+    The functions below take it, or any four tensors like these."""
+    k: torch.Tensor          # int8 [num_pages, kv_heads, page_size, head_dim]
+    v: torch.Tensor
+    k_scale: torch.Tensor    # float32 [num_pages, kv_heads]
+    v_scale: torch.Tensor
+
+    @staticmethod
+    def allocate(num_pages: int, kv_heads: int, page_size: int, head_dim: int, device) -> "PagedCache":
+        codes = [torch.zeros((num_pages, kv_heads, page_size, head_dim), dtype=torch.int8, device=device) for _ in range(2)]
+        scales = [torch.zeros((num_pages, kv_heads), dtype=torch.float32, device=device) for _ in range(2)]
+        return PagedCache(*codes, *scales)
+
+
+class PageMap(NamedTuple):
+    """What map_pages fills, int32: slot_map and positions of every row (-1: a row of no request), seq_lens of every request,
+    state = (entry of the free list to go on from, DEV_* bits)."""
+    slot_map: torch.Tensor
+    positions: torch.Tensor
+    seq_lens: torch.Tensor
+    state: torch.Tensor
+
+    @staticmethod
+    def allocate(total_rows: int, batch: int, device) -> "PageMap":
+        return PageMap(*(torch.empty(n, dtype=torch.int32, device=device) for n in (total_rows, total_rows, batch, 2)))
+
+
+_CODE = {torch.bfloat16: BF16, torch.float32: FP32}
+
+
+def _on_device(device: torch.device, stream: Optional[torch.cuda.Stream], where: str, call, *args) -> None:
+    """call(stream handle, *args) with `device` current."""
+    if device.index == torch._C._cuda_getDevice():
+        _check(call(_stream_handle(stream), *args), where)
+    else:
+        with torch.cuda.device(device):
+            _check(call(_stream_handle(stream), *args), where)
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _int32(t: torch.Tensor, n: int, device: torch.device, what: str) -> int:
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < n or t.device != device:
+        raise ValueError("%s must be a contiguous int32 tensor of at least %d on %s" % (what, n, device))
+    return t.data_ptr()
+
+
+def _heads(t: torch.Tensor, rows: int, device: torch.device, what: str) -> int:
+    """Row stride, in elements, of [rows, heads, head_dim] with heads back to back."""
+    if t.dim() != 3 or t.shape[0] != rows or t.device != device or (rows and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]))):
+        raise ValueError("%s must be [%d, heads, head_dim] on %s, the heads of a row back to back" % (what, rows, device))
+    return t.stride(0) if rows > 1 else t.shape[1] * t.shape[2]
+
+
+def _ccache(cache) -> CCache:
+    k, v, ks, vs = cache
+    if (k.dim() != 4 or k.shape != v.shape or k.dtype != torch.int8 or v.dtype != torch.int8 or not k.is_contiguous()
+            or not v.is_contiguous() or ks.dtype != torch.float32 or vs.dtype != torch.float32 or ks.shape != k.shape[:2]
+            or vs.shape != ks.shape or not ks.is_contiguous() or not vs.is_contiguous()
+            or not k.is_cuda or v.device != k.device or ks.device != k.device or vs.device != k.device):
+        raise ValueError("a cache is int8 codes k, v [pages, kv_heads, page_size, head_dim] and float32 scales [pages, kv_heads], "
+                         "contiguous, on one CUDA device")
+    pages, heads, page, dim = k.shape
+    return CCache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, page, heads, dim)
+
+
+def rope_frequencies(rotary_dim: int, theta: float, device) -> torch.Tensor:
+    """theta^(-2p / rotary_dim) for the pairs p of qk_norm_rope, float64."""
+    return theta ** (torch.arange(0, rotary_dim, 2, dtype=torch.float64, device=device) / -rotary_dim)
+
+
+def map_pages(offsets: torch.Tensor, block_tables: torch.Tensor, free_pages: torch.Tensor, free_head: torch.Tensor, out, *,
+              page_size: int, context_lens: Optional[torch.Tensor] = None, token_index: Optional[torch.Tensor] = None,
+              position_base: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """rtprune_page_map: hands pages of the free list to a ragged batch's new tokens, on the device.  `offsets` [batch + 1] and
+    `token_index` are a run's out_offsets and kept_idx; `block_tables` [batch, max_pages] gets the new pages' entries; `out` is a
+    PageMap (or four tensors like it), of as many rows as `out.slot_map` has."""
+    slots, positions, lens, state = out
+    dev, batch = offsets.device, offsets.numel() - 1
+    _need(offsets.is_cuda and batch >= 0, "offsets must be [batch + 1] on a CUDA device")
+    rows = slots.numel()
+    _need(block_tables.dtype == torch.int32 and block_tables.dim() == 2 and block_tables.shape[0] == batch and block_tables.device == dev
+          and (block_tables.shape[1] <= 1 or block_tables.stride(1) == 1), "block_tables must be int32 [batch, max_pages], rows contiguous")
+    pages = block_tables.shape[1]
+    _on_device(dev, stream, "rtprune_page_map", lib().rtprune_page_map, _int32(offsets, batch + 1, dev, "offsets"),
+               None if context_lens is None else _int32(context_lens, batch, dev, "context_lens"), batch, rows,
+               None if token_index is None else _int32(token_index, rows, dev, "token_index"),
+               None if position_base is None else _int32(position_base, batch, dev, "position_base"),
+               _int32(free_pages, 0, dev, "free_pages"), _int32(free_head, 1, dev, "free_head"), free_pages.numel(), page_size,
+               block_tables.data_ptr(), block_tables.stride(0) if batch > 1 else pages, pages, _int32(slots, 0, dev, "slot_map"),
+               None if positions is None else _int32(positions, rows, dev, "positions"), _int32(lens, batch, dev, "seq_lens"),
+               _int32(state, 2, dev, "state"))
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor,
+                 q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, *,
+                 interleaved: bool = False, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None) -> None:
+    """rtprune_qk_norm_rope on q [rows, q_heads, head_dim] and k [rows, kv_heads, head_dim] (bf16 or float32; rows may be parts of
+    a fused projection's).  In place unless q_out, k_out are given.  The rotated part is 2 * inv_freq.numel() wide."""
+    dev, rows = q.device, q.shape[0]
+    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
+    dim, dtype = q.shape[-1], q.dtype
+    _need(q.is_cuda and dtype in _CODE, "q must be bf16 or float32 on a CUDA device")
+    for t in (k, q_out, k_out):
+        _need(t.dtype == dtype and t.shape[-1] == dim, "q, k and the outputs must have one dtype and head_dim")
+    _need(q_out.shape == q.shape and k_out.shape == k.shape, "the outputs must have the inputs' shapes")
+    for w in (q_weight, k_weight):
+        _need(w is None or (w.dtype == dtype and w.numel() == dim and w.is_contiguous() and w.device == dev), "weights must be [head_dim] like q")
+    _need(inv_freq.dtype == torch.float64 and inv_freq.is_contiguous() and inv_freq.device == dev, "inv_freq must be contiguous float64 on q's device")
+    _on_device(dev, stream, "rtprune_qk_norm_rope", lib().rtprune_qk_norm_rope, _CODE[dtype], q.data_ptr(), _heads(q, rows, dev, "q"),
+               k.data_ptr(), _heads(k, rows, dev, "k"), rows, q.shape[1], k.shape[1], dim, _ptr(q_weight), _ptr(k_weight), eps,
+               _int32(positions, rows, dev, "positions"), inv_freq.data_ptr(), 2 * inv_freq.numel(), int(interleaved),
+               q_out.data_ptr(), _heads(q_out, rows, dev, "q_out"), k_out.data_ptr(), _heads(k_out, rows, dev, "k_out"))
+
+
+def cache_write(k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, cache, *, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """rtprune_cache_write: k, v [rows, kv_heads, head_dim] (bf16 or float32) to the slots of a PagedCache; rows with slot -1 go nowhere."""
+    c, dev, rows = _ccache(cache), cache[0].device, k.shape[0]
+    _need(k.dtype in _CODE and v.dtype == k.dtype, "k and v must both be bf16 or both float32")
+    _need(k.shape == v.shape and k.shape[1:] == (c.kv_heads, c.head_dim), "k and v must be [rows, kv_heads, head_dim] of the cache")
+    _on_device(dev, stream, "rtprune_cache_write", lib().rtprune_cache_write, _CODE[k.dtype], k.data_ptr(), _heads(k, rows, dev, "k"),
+               v.data_ptr(), _heads(v, rows, dev, "v"), rows, _int32(slot_map, rows, dev, "slot_map"), c)
+
+
+def cache_attend(q: torch.Tensor, offsets: torch.Tensor, seq_lens: torch.Tensor, block_tables: torch.Tensor, cache, *, max_q_len: int,
+                 max_seq_len: int, scale: Optional[float] = None, causal: bool = True, out: Optional[torch.Tensor] = None,
+                 lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """rtprune_cache_attend: bf16 queries [rows, q_heads, head_dim], the last offsets[i+1] - offsets[i] tokens of request i each,
+    over the seq_lens[i] tokens that it has in the cache.  scale: head_dim^-1/2 unless given.  Returns `out` (bf16, zeros where no
+    tensor was given); `lse` float32 [rows, q_heads] is filled if given.  `workspace`: cache_attend_workspace bytes of the caller's,
+    else the call takes them from torch's allocator on its stream."""
+    c, dev, rows = _ccache(cache), cache[0].device, q.shape[0]
+    batch = offsets.numel() - 1
+    if stream is not None and (out is None or workspace is None):
+        with torch.cuda.stream(stream):        # memory taken here belongs to the stream that uses it
+            return cache_attend(q, offsets, seq_lens, block_tables, cache, max_q_len=max_q_len, max_seq_len=max_seq_len, scale=scale,
+                                causal=causal, out=out, lse=lse, workspace=workspace)
+    _need(q.dtype == torch.bfloat16 and q.dim() == 3 and q.shape[2] == c.head_dim, "q must be bf16 [rows, q_heads, head_dim of the cache]")
+    stride, heads = _heads(q, rows, dev, "q"), q.shape[1]
+    if out is None:
+        out = torch.zeros((rows, heads, c.head_dim), dtype=torch.bfloat16, device=dev)
+    _need(out.dtype == torch.bfloat16 and out.shape == q.shape and out.is_contiguous() and out.device == dev, "out must be contiguous bf16 of q's shape")
+    _need(lse is None or (lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous() and lse.device == dev),
+          "lse must be contiguous float32 [rows, q_heads]")
+    _need(block_tables.dtype == torch.int32 and block_tables.dim() == 2 and block_tables.shape[0] == batch and block_tables.device == dev
+          and (block_tables.shape[1] <= 1 or block_tables.stride(1) == 1), "block_tables must be int32 [batch, max_pages], rows contiguous")
+    if workspace is None:
+        workspace = torch.empty(cache_attend_workspace(batch, max_q_len, max_seq_len, heads, c.kv_heads, c.head_dim),
+                                dtype=torch.uint8, device=dev)
+    _need(workspace.device == dev and workspace.is_contiguous(), "the workspace must be contiguous on the cache's device")
+    pages = block_tables.shape[1]
+    _on_device(dev, stream, "rtprune_cache_attend", lib().rtprune_cache_attend, q.data_ptr(), stride, rows, heads,
+               _int32(offsets, batch + 1, dev, "offsets"), _int32(seq_lens, batch, dev, "seq_lens"), batch, max_q_len, max_seq_len,
+               block_tables.data_ptr(), block_tables.stride(0) if batch > 1 else pages, pages, c,
+               c.head_dim ** -0.5 if scale is None else scale, int(causal), out.data_ptr(), _ptr(lse), workspace.data_ptr(),
+               workspace.numel() * workspace.element_size())
+    return out
+
+
+def cache_attend_workspace(batch: int, max_q_len: int, max_seq_len: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    """rtprune_cache_attend_workspace: bytes of workspace a cache_attend of these sizes needs."""
+    n = ctypes.c_size_t()
+    _check(lib().rtprune_cache_attend_workspace(batch, max_q_len, max_seq_len, q_heads, kv_heads, head_dim, ctypes.byref(n)),
+           "rtprune_cache_attend_workspace")
+    return n.value
 
 
 def shard_images(batch: int, world_size: int, rank: int):
