@@ -1,46 +1,12 @@
 // Attention over the 8-bit paged cache (rtprune_cache_attend).
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
-#include "serve.cuh"
+#include "attend.cuh"
+#include "attend_rows.cuh"
 
 namespace rtp {
-
-// Row r of request i, its j-th of n_i, sees the cached tokens t < end: L_i, or L_i - n_i + j + 1 when causal.
-//   s_t = scale * ks * (q . kc_t),  out = sum_t softmax(s)_t vs vc_t,  lse = log sum_t exp s_t
-// with kc, vc the codes of token t and ks, vs the scales of its page and head.
-struct AttendArgs {
-    const __nv_bfloat16 *q;
-    int64_t q_stride;
-    const int32_t *offsets, *seq_lens, *tables;
-    int64_t table_stride;
-    int32_t batch, rows, q_heads, group, max_q_len, max_len, max_pages;
-    CacheView c;
-    float scale_log2;                        // scale * log2(e): the softmax runs in powers of two
-    int32_t causal;
-    __nv_bfloat16 *out;
-    float *lse;
-};
-
-// A request's rows and lengths, checked.  false: no rows of it can be written.  `len` < 0: outside the contract, its rows come out NaN.
-__device__ inline bool attend_request(const AttendArgs &a, int i, int &row0, int &n, int &len)
-{
-    row0 = __ldg(a.offsets + i);
-    const int hi = __ldg(a.offsets + i + 1);
-    n = hi - row0;
-    len = __ldg(a.seq_lens + i);
-    if (row0 < 0 || n <= 0 || hi > a.rows || n > a.max_q_len) return false;
-    if (len < 0 || len > a.max_len) len = -1;
-    return true;
-}
-
-// The page of token t, or -1.
-__device__ inline int attend_page(const AttendArgs &a, int i, int t)
-{
-    const int p = t >> a.c.page_shift;
-    const int page = p < a.max_pages ? __ldg(a.tables + (int64_t)i * a.table_stride + p) : -1;
-    return page < a.c.num_pages ? page : -1;
-}
 
 constexpr int kAtWarps = 4;
 
@@ -85,6 +51,54 @@ attend_simple_kernel(const __grid_constant__ AttendArgs a)
         a.lse[row * a.q_heads + head] = nan ? inv : end > 0 ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
 }
 
+constexpr int kAtFewRows = 64;               // rows of a kv head up to which attend_rows_kernel takes the call
+
+// Workspace of attend_rows_kernel with `ctas` CTAs.
+struct RowsLayout {
+    size_t part, part_ml, join, total;
+};
+static RowsLayout rows_layout(int ctas, int dim)
+{
+    RowsLayout w;
+    w.part = 0;
+    w.part_ml = w.part + (size_t)2 * ctas * kArRows * dim * 4;
+    w.join = w.part_ml + (size_t)2 * ctas * kArRows * 8;
+    w.total = w.join + (size_t)ctas * 16;
+    return w;
+}
+
+// The kernel's dynamic shared memory, set once on each device (a bit of the mask).
+template <typename K> static cudaError_t allow_smem(K kernel, int bytes, std::atomic<unsigned long long> &ready)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev < 64 && (ready.load(std::memory_order_relaxed) >> dev & 1))) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+    return e;
+}
+
+static int device_sms()
+{
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return sms;
+}
+
+template <int D>
+static cudaError_t launch_rows(const AttendArgs &a, int ctas, uint8_t *ws, cudaStream_t st)
+{
+    const RowsLayout w = rows_layout(ctas, D);
+    static std::atomic<unsigned long long> ready{0};             // devices that know the kernel's shared memory
+    cudaError_t e = allow_smem(attend_rows_kernel<D>, ArShape<D>::kSmem, ready);
+    if (e != cudaSuccess) return e;
+    e = launch_chained(attend_rows_kernel<D>, dim3(ctas), dim3(kArThreads), (size_t)ArShape<D>::kSmem, st, a, (float *)(ws + w.part),
+                       (float2 *)(ws + w.part_ml), (int4 *)(ws + w.join));
+    if (e != cudaSuccess) return e;
+    return launch_chained(attend_join_kernel<D>, dim3(ctas), dim3(kArRows * D / 4), (size_t)0, st, a, (const float *)(ws + w.part),
+                          (const float2 *)(ws + w.part_ml), (const int4 *)(ws + w.join));
+}
+
 }  // namespace rtp
 
 extern "C" rtprune_status_t rtprune_cache_attend_workspace(int32_t batch, int32_t max_q_len, int64_t max_seq_len, int32_t q_heads,
@@ -93,6 +107,8 @@ extern "C" rtprune_status_t rtprune_cache_attend_workspace(int32_t batch, int32_
     if (!workspace_bytes || batch < 0 || max_q_len < 0 || max_seq_len < 0 || q_heads <= 0 || kv_heads <= 0 || head_dim <= 0)
         return RTPRUNE_ERR_INVALID_ARG;
     *workspace_bytes = 256;
+    if ((int64_t)max_q_len * (q_heads / kv_heads) <= rtp::kAtFewRows)
+        *workspace_bytes = rtp::rows_layout(rtp::kArMostCtas, head_dim).total;
     return RTPRUNE_OK;
 }
 
@@ -122,6 +138,15 @@ extern "C" rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *
     AttendArgs a = {(const __nv_bfloat16 *)q, q_stride, offsets, seq_lens, block_tables, table_stride, batch, (int)rows, q_heads,
                     q_heads / c.kv_heads, max_q_len, (int)max_seq_len, max_pages, c, scale * 1.4426950408889634f, causal ? 1 : 0,
                     (__nv_bfloat16 *)out, lse};
+    if ((int64_t)max_q_len * a.group <= kAtFewRows) {
+        const int ctas = std::min(kArPerSm * device_sms(), kArMostCtas);
+        if (!ctas) return RTPRUNE_ERR_CUDA;
+        uint8_t *ws = (uint8_t *)workspace;
+        const cudaError_t e = c.dim == 128 ? launch_rows<128>(a, ctas, ws, (cudaStream_t)cuda_stream)
+                                           : launch_rows<64>(a, ctas, ws, (cudaStream_t)cuda_stream);
+        if (e != cudaSuccess) return RTPRUNE_ERR_CUDA;
+        return cudaGetLastError() == cudaSuccess ? RTPRUNE_OK : RTPRUNE_ERR_CUDA;
+    }
     const dim3 grid((unsigned)((max_q_len + kAtWarps - 1) / kAtWarps), (unsigned)q_heads, (unsigned)batch);
     if (launch_chained(attend_simple_kernel, grid, dim3(32 * kAtWarps), (size_t)0, (cudaStream_t)cuda_stream, a) != cudaSuccess)
         return RTPRUNE_ERR_CUDA;

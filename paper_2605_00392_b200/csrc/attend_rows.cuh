@@ -1,0 +1,515 @@
+// Attention of few query rows per kv head (single tokens, a few drafted ones) over the 8-bit paged cache: bound by reading
+// the codes once.
+//
+// A tile of 16 rows (a token's heads of one kv head, token by token) against 64 tokens a step, a warp 16 of them, on
+// mma.sync m16n8k16: at one or a few rows the tensor cores are idle either way (a step of 8 KB and 16 rows has 0.3 us of HBM
+// time per SM and 0.02 of mma), and its fragments come straight out of 16-byte loads because both contractions may run in any order:
+//   scores  a lane takes 32 (D = 64: 16) neighbouring elements of a token's key; the queries' fragments are laid out to match
+//   values  a lane takes 16 (8) neighbouring columns of four tokens: n-tile j of the output is column 16 g + j of each lane group g
+// Codes come through a warp's own ring of cp.async stages in shared memory, 16-byte pieces swizzled by row so that both ways of reading
+// are free of conflicts; the scales of a stage's block come with it.
+//
+// The work, all (request, kv head, tile of rows) with their blocks of 64 tokens, is one line that is cut into equal runs, one per CTA
+// (three to an SM), whatever the requests' lengths: each CTA sums up the batch for itself and finds its place.  A tile that a cut goes through is
+// left in parts (fp32 sums, m', l) that attend_join_kernel puts together in the order of the line, so results do not depend on timing.
+// The ring runs across tiles: the next one's codes are on their way while this one's warps are added up.
+#pragma once
+#include "attend.cuh"
+
+namespace rtp {
+
+constexpr int kArWarps = 4;
+constexpr int kArThreads = 32 * kArWarps;
+constexpr int kArBlock = 16 * kArWarps;              // tokens of a step
+constexpr int kArPerSm = 3;                          // CTAs of an SM
+constexpr int kArMostCtas = kArPerSm * 160;          // what the workspace is sized for (a B200 has 148 SMs)
+constexpr int kArRows = 16;
+constexpr int kArLeast = 4;                          // blocks of a run at least
+
+template <int D> struct ArShape {
+    static constexpr int kStages = D == 128 ? 3 : 6;
+    static constexpr int kTile = 16 * D;             // bytes of a warp's keys (or values) of a stage
+    static constexpr int kSteps = D / 16;            // mma steps of a score
+    static constexpr int kNt = D / 8;                // n-tiles of the output
+    static constexpr int kRing = kArWarps * kStages * 2 * kTile;
+    static constexpr int kFrag = kSteps * 32 * 16;   // the queries' fragments
+    static constexpr int kJoin = (kArWarps / 2) * 32 * kNt * 16;   // accumulators of half the warps
+    static constexpr int kSmem = kRing + kFrag + kJoin + kArWarps * kStages * 8;
+};
+
+// A place in the line of work.
+struct ArPlace {
+    int i, head, tile, block;                        // request, kv head, tile of rows, block of tokens
+    int row0, n, len, blocks, tiles;                 // of the request
+
+    __device__ void request(const AttendArgs &a, int at)
+    {
+        i = at;
+        head = tile = block = 0;
+        tiles = 0;
+        if (i < a.batch && attend_request(a, i, row0, n, len)) {
+            tiles = (n * a.group + kArRows - 1) / kArRows;
+            blocks = max(1, (len + kArBlock - 1) / kArBlock);
+        }
+    }
+    // (the line ends before the batch does: the caller counts)
+    __device__ void next(const AttendArgs &a)
+    {
+        if (++block < blocks) return;
+        block = 0;
+        if (++tile < tiles) return;
+        tile = 0;
+        if (++head < a.c.kv_heads) return;
+        do request(a, i + 1);
+        while (tiles == 0 && i < a.batch);
+    }
+};
+
+__device__ inline int64_t ar_units(const AttendArgs &a, int i)
+{
+    int row0, n, len;
+    if (!attend_request(a, i, row0, n, len)) return 0;
+    return (int64_t)((n * a.group + kArRows - 1) / kArRows) * a.c.kv_heads * max(1, (len + kArBlock - 1) / kArBlock);
+}
+
+// Where CTA `blockIdx.x` of the line begins, and how many blocks it takes (0: none).
+__device__ inline int ar_find(const AttendArgs &a, ArPlace &at, int &chunk)
+{
+    __shared__ int64_t warp_units[kArWarps], found_before;
+    __shared__ int found;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (a.batch + kArThreads - 1) / kArThreads, i0 = min(tid * per, a.batch), i1 = min(i0 + per, a.batch);
+    int64_t mine = 0;
+    for (int i = i0; i < i1; ++i) mine += ar_units(a, i);
+    int64_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t t = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += t;
+    }
+    if (lane == 31) warp_units[warp] = upto;
+    __syncthreads();
+    int64_t total = 0, before = upto - mine;
+#pragma unroll
+    for (int w = 0; w < kArWarps; ++w) {
+        if (w < warp) before += warp_units[w];
+        total += warp_units[w];
+    }
+    const int64_t run = max((total + gridDim.x - 1) / gridDim.x, (int64_t)kArLeast);
+    const int64_t start = run * blockIdx.x;
+    chunk = (int)run;
+    if (start >= total) return 0;
+    if (start >= before && start < before + mine) {
+        int i = i0;
+        for (int64_t u; (u = ar_units(a, i)) <= start - before; ++i) before += u;
+        found = i;
+        found_before = before;
+    }
+    __syncthreads();
+    at.request(a, found);
+    const int64_t rel = start - found_before;
+    at.block = (int)(rel % at.blocks);
+    at.tile = (int)(rel / at.blocks % at.tiles);
+    at.head = (int)(rel / at.blocks / at.tiles);
+    return (int)min(run, total - start);
+}
+
+__device__ inline void mma_f16(float (&d)[4], const uint4 &a, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+}
+__device__ inline uint4 lds_v4(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+__device__ inline uint2 lds_v2(uint32_t at)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+    return v;
+}
+__device__ inline float2 lds_f2(uint32_t at)
+{
+    float2 v;
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at));
+    return v;
+}
+__device__ inline void cp_async_4(uint32_t dst_smem, const void *src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst_smem), "l"(src) : "memory");
+}
+
+// Place of 16-byte piece `ch` of row t of a tile.
+template <int D> __device__ inline uint32_t ar_piece(int t, int ch)
+{
+    if (D == 128) return (uint32_t)(t * 128 + ((ch ^ (t & 7)) << 4));
+    const int line = t >> 1;
+    return (uint32_t)(line * 128 + ((((t & 1) * 4 + ch) ^ ((line & 3) << 1)) << 4));
+}
+
+// Parts of a tile that a cut goes through: `part` [2 per CTA][16][D] sums, `part_ml` [2 per CTA][16] (m', l).  A part that holds its
+// tile's first block is the CTA's second, any other its first.  join[CTA]: the tile that begins in the CTA and does not end in it:
+// (first row of the request, kv head, the tile's first row | its rows << 26, CTAs that it goes through; 0: there is none).
+template <int D>
+__global__ void __launch_bounds__(kArThreads, kArPerSm)
+attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ part, float2 *__restrict__ part_ml,
+                   int4 *__restrict__ join)
+{
+    using S = ArShape<D>;
+    extern __shared__ __align__(128) uint8_t sm[];
+    __shared__ float row_factor[kArRows];
+    __shared__ float2 row_ml[kArWarps][kArRows];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+    const uint32_t ring = ptx::smem_u32(sm) + warp * S::kStages * 2 * S::kTile;
+    const uint32_t frag = ptx::smem_u32(sm) + S::kRing;
+    const uint32_t scales = frag + S::kFrag + S::kJoin + warp * S::kStages * 8;
+    float4 *joined = reinterpret_cast<float4 *>(sm + S::kRing + S::kFrag);
+    ptx::grid_dep_launch();
+    ptx::grid_dep_wait();
+    ArPlace at, ahead;
+    int chunk;
+    const int todo = ar_find(a, at, chunk);
+    if (todo == 0) {
+        if (tid == 0) join[blockIdx.x] = make_int4(0, 0, 0, 0);
+        return;
+    }
+    ahead = at;
+
+    // the next block's codes of this warp (16 tokens) on their way into stage s
+    int ahead_left = todo, stage_in = 0;
+    auto fetch = [&]() {
+        if (ahead_left > 0) {
+            const int t0 = ahead.block * kArBlock + warp * 16;
+            if (t0 < ahead.len) {
+                const int page = attend_page(a, ahead.i, t0);
+                const int64_t block = (int64_t)max(page, 0) * a.c.kv_heads + ahead.head;
+                const int64_t from = (block * a.c.page_size + (t0 & (a.c.page_size - 1))) * D;
+                const uint32_t to = ring + stage_in * 2 * S::kTile;
+#pragma unroll
+                for (int p = 0; p < D / 32; ++p) {
+                    const int piece = lane + 32 * p, t = piece / (D / 16), ch = piece % (D / 16);
+                    ptx::cp_async_16(to + ar_piece<D>(t, ch), a.c.k + from + piece * 16, 16);
+                    ptx::cp_async_16(to + S::kTile + ar_piece<D>(t, ch), a.c.v + from + piece * 16, 16);
+                }
+                if (lane < 2) {
+                    const uint32_t s_to = scales + stage_in * 8 + lane * 4;
+                    if (page >= 0) cp_async_4(s_to, (lane ? a.c.v_scale : a.c.k_scale) + block);
+                    else asm volatile("st.shared.b32 [%0], %1;" ::"r"(s_to), "r"(0x7fc00000u) : "memory");
+                }
+            }
+            --ahead_left;
+            ahead.next(a);
+        }
+        ptx::cp_async_commit();
+        if (++stage_in == S::kStages) stage_in = 0;
+    };
+#pragma unroll
+    for (int s = 0; s < S::kStages - 1; ++s) fetch();
+
+    int stage = 0;
+    for (int left = todo; left > 0;) {
+        // ---- a tile of rows: its queries as fragments
+        const int first = at.block, steps = min(left, at.blocks - at.block), rows = at.n * a.group;
+        __syncthreads();                             // the last tile's fragments and sums have been read
+        {
+            constexpr int kPer = D / 8;              // elements of a thread: 8 threads a row
+            const int r = tid >> 3, k = tid & 7, m = at.tile * kArRows + r;
+            uint4 raw[kPer / 8];
+#pragma unroll
+            for (int e = 0; e < kPer / 8; ++e) raw[e] = make_uint4(0u, 0u, 0u, 0u);
+            if (m < rows) {
+                const int j = m / a.group, h = at.head * a.group + (m - j * a.group);
+                const uint4 *p = reinterpret_cast<const uint4 *>(a.q + (int64_t)(at.row0 + j) * a.q_stride + (int64_t)h * D + k * kPer);
+#pragma unroll
+                for (int e = 0; e < kPer / 8; ++e) raw[e] = __ldg(p + e);
+            }
+            float f[kPer], top = 0.f;
+#pragma unroll
+            for (int e = 0; e < kPer / 8; ++e) {
+                float t8[8];
+                Elem<__nv_bfloat16>::unpack(raw[e], t8);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    f[8 * e + x] = t8[x];
+                    top = max_nan(top, fabsf(t8[x]));
+                }
+            }
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+            float factor;
+            const float unit = query_scale(top, a.scale_log2, factor);
+            if (k == 0) row_factor[r] = factor;
+            // element d: lane (r & 7) * 4 + d / (D / 4), step (d mod D / 4) / 4, register (d & 2) + (r >= 8)
+#pragma unroll
+            for (int e = 0; e < kPer; e += 2) {
+                const int d = k * kPer + e, lane_to = (r & 7) * 4 + d / (D / 4), step = d % (D / 4) / 4;
+                const uint32_t to = frag + (uint32_t)((step * 32 + lane_to) * 16 + ((d & 2) + (r >> 3)) * 4);
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(to), "r"(pack_half(f[e] * unit, f[e + 1] * unit)) : "memory");
+            }
+        }
+        __syncthreads();
+        // ends of this lane's two rows, of the tile's first and last one
+        int end[2], lo_end, hi_end;
+        {
+            const int m0 = at.tile * kArRows, last = min(m0 + kArRows, rows) - 1, len = max(at.len, 0), past = len - at.n + 1;
+            end[0] = a.causal ? min(len, past + min(m0 + g, last) / a.group) : len;
+            end[1] = a.causal ? min(len, past + min(m0 + g + 8, last) / a.group) : len;
+            lo_end = a.causal ? min(len, past + m0 / a.group) : len;
+            hi_end = a.causal ? min(len, past + last / a.group) : len;
+        }
+        const float f0 = row_factor[g], f1 = row_factor[g + 8];
+        float acc[S::kNt][4], m[2] = {kAtNothing, kAtNothing}, l[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < S::kNt; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+
+        for (int b = 0; b < steps; ++b) {
+            ptx::cp_async_wait<S::kStages - 2>();
+            __syncwarp();                            // everyone's pieces are there; everyone is done with the stage before
+            fetch();
+            const int t0 = (first + b) * kArBlock + warp * 16;
+            const uint32_t kt = ring + stage * 2 * S::kTile, vt = kt + S::kTile;
+            const float2 sc = lds_f2(scales + stage * 8);
+            if (++stage == S::kStages) stage = 0;
+            if (t0 >= hi_end) continue;
+            // ---- scores of tokens t0 + 2c, 2c + 1 (s[0]) and 8 more (s[1]) for rows g, g + 8
+            float s[2][4] = {};
+#pragma unroll
+            for (int h = 0; h < D / 64; ++h) {
+                uint32_t w[2][4];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const uint4 v = lds_v4(kt + ar_piece<D>(g + 8 * x, D == 128 ? 2 * c + h : c));
+                    w[x][0] = v.x ^ 0x80808080u;
+                    w[x][1] = v.y ^ 0x80808080u;
+                    w[x][2] = v.z ^ 0x80808080u;
+                    w[x][3] = v.w ^ 0x80808080u;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint4 qf = lds_v4(frag + (uint32_t)(((h * 4 + e) * 32 + lane) * 16));
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        uint32_t b0, b1;
+                        codes_to_half(w[x][e], b0, b1);
+                        mma_f16(s[x], qf, b0, b1);
+                    }
+                }
+            }
+            // ---- weights
+            float lv, inv;
+            value_scale(sc.y, lv, inv);
+            const float k0 = f0 * sc.x, k1 = f1 * sc.x;
+            const bool masked = t0 + 16 > lo_end;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[x][e] = fmaf(s[x][e], e < 2 ? k0 : k1, lv);
+                    if (masked && t0 + 8 * x + 2 * c + (e & 1) >= end[e >> 1]) s[x][e] = -INFINITY;
+                }
+            }
+            const float top0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
+            const float top1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
+            if (__any_sync(0xffffffffu, top0 - m[0] > kAtSlack || top1 - m[1] > kAtSlack)) {
+                float n0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, 1)), n1 = fmaxf(top1, __shfl_xor_sync(0xffffffffu, top1, 1));
+                n0 = fmaxf(m[0], fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, 2)));
+                n1 = fmaxf(m[1], fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, 2)));
+                const float c0 = ex2(m[0] - n0), c1 = ex2(m[1] - n1);
+                m[0] = n0;
+                m[1] = n1;
+                l[0] *= c0;
+                l[1] *= c1;
+#pragma unroll
+                for (int j = 0; j < S::kNt; ++j) {
+                    acc[j][0] *= c0;
+                    acc[j][1] *= c0;
+                    acc[j][2] *= c1;
+                    acc[j][3] *= c1;
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = ex2(s[x][e] - m[e >> 1]);
+                    // a weight of 0 by the mask adds nothing, whatever its block's scale is
+                    if (!masked || s[x][e] != -INFINITY) l[e >> 1] = fmaf(p, inv, l[e >> 1]);
+                    s[x][e] = p;
+                }
+            const uint4 pf = make_uint4(pack_half(s[0][0], s[0][1]), pack_half(s[0][2], s[0][3]), pack_half(s[1][0], s[1][1]),
+                                        pack_half(s[1][2], s[1][3]));
+            // ---- values: tokens 2c, 2c + 1, 2c + 8, 2c + 9, columns D / 8 * g ..
+            uint32_t v[4][D / 32];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int t = 2 * c + (x & 1) + 8 * (x >> 1);
+                if (D == 128) {
+                    const uint4 r = lds_v4(vt + ar_piece<D>(t, g));
+                    v[x][0] = r.x ^ 0x80808080u;
+                    v[x][1] = r.y ^ 0x80808080u;
+                    v[x][D / 32 - 2] = r.z ^ 0x80808080u;
+                    v[x][D / 32 - 1] = r.w ^ 0x80808080u;
+                } else {
+                    const uint2 r = lds_v2(vt + ar_piece<D>(t, g >> 1) + (g & 1) * 8);
+                    v[x][0] = r.x ^ 0x80808080u;
+                    v[x][1] = r.y ^ 0x80808080u;
+                }
+            }
+#pragma unroll
+            for (int w = 0; w < D / 32; ++w) {
+                uint32_t b0[4], b1[4];
+                codes_to_half(__byte_perm(v[0][w], v[1][w], 0x5140), b0[0], b0[1]);
+                codes_to_half(__byte_perm(v[0][w], v[1][w], 0x7362), b0[2], b0[3]);
+                codes_to_half(__byte_perm(v[2][w], v[3][w], 0x5140), b1[0], b1[1]);
+                codes_to_half(__byte_perm(v[2][w], v[3][w], 0x7362), b1[2], b1[3]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mma_f16(acc[4 * w + j], pf, b0[j], b1[j]);
+            }
+        }
+
+        // ---- the warps' sums, put together in their order: to a common m', then 2 + 2, then 1 + 1
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            l[x] += __shfl_xor_sync(0xffffffffu, l[x], 1);
+            l[x] += __shfl_xor_sync(0xffffffffu, l[x], 2);
+            if (c == 0) row_ml[warp][g + 8 * x] = make_float2(m[x], l[x]);
+        }
+        __syncthreads();
+        float sum_l[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            float top = kAtNothing;
+#pragma unroll
+            for (int w = 0; w < kArWarps; ++w) top = fmaxf(top, row_ml[w][g + 8 * x].x);
+            sum_l[x] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kArWarps; ++w) {
+                const float2 ml = row_ml[w][g + 8 * x];
+                sum_l[x] += ml.y * ex2(ml.x - top);
+            }
+            const float k = ex2(m[x] - top);
+            m[x] = top;
+#pragma unroll
+            for (int j = 0; j < S::kNt; ++j) {
+                acc[j][2 * x] *= k;
+                acc[j][2 * x + 1] *= k;
+            }
+        }
+#pragma unroll
+        for (int half = kArWarps / 2; half > 0; half >>= 1) {
+            if (warp >= half && warp < 2 * half) {
+#pragma unroll
+                for (int j = 0; j < S::kNt; ++j)
+                    joined[((warp - half) * S::kNt + j) * 32 + lane] = make_float4(acc[j][0], acc[j][1], acc[j][2], acc[j][3]);
+            }
+            __syncthreads();
+            if (warp < half) {
+#pragma unroll
+                for (int j = 0; j < S::kNt; ++j) {
+                    const float4 o = joined[(warp * S::kNt + j) * 32 + lane];
+                    acc[j][0] += o.x;
+                    acc[j][1] += o.y;
+                    acc[j][2] += o.z;
+                    acc[j][3] += o.w;
+                }
+            }
+            if (half > 1) __syncthreads();
+        }
+        const bool whole = first == 0 && steps == at.blocks;
+        if (warp == 0) {
+            // lane (g, c) has columns D / 4 * c .. of rows g, g + 8: column n-tile j, c0 / c1 = j / j + D / 8
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int r = g + 8 * x, mr = at.tile * kArRows + r;
+                if (mr >= rows) continue;
+                const int slot = 2 * blockIdx.x + (first == 0 ? 1 : 0);
+                if (whole) {
+                    const bool nan = at.len < 0;
+                    const float k = nan ? __uint_as_float(0x7fc00000u) : sum_l[x] == 0.f ? 0.f : 1.f / sum_l[x];
+                    const int j = mr / a.group;
+                    const int64_t o = (int64_t)(at.row0 + j) * a.q_heads + at.head * a.group + (mr - j * a.group);
+                    __nv_bfloat16 *to = a.out + o * D + c * (D / 4);
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+#pragma unroll
+                        for (int e = 0; e < D / 8; e += 8) {
+                            uint4 w;
+                            __nv_bfloat162 *h = reinterpret_cast<__nv_bfloat162 *>(&w);
+#pragma unroll
+                            for (int z = 0; z < 4; ++z)
+                                h[z] = __floats2bfloat162_rn(acc[e + 2 * z][2 * x + y] * k, acc[e + 2 * z + 1][2 * x + y] * k);
+                            *reinterpret_cast<uint4 *>(to + y * (D / 8) + e) = w;
+                        }
+                    if (a.lse && c == 0)
+                        a.lse[o] = nan ? k : sum_l[x] == 0.f ? -INFINITY : (m[x] + log2f(sum_l[x])) * kAtLn2;
+                } else {
+                    float *to = part + ((int64_t)slot * kArRows + r) * D + c * (D / 4);
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+#pragma unroll
+                        for (int e = 0; e < D / 8; e += 4)
+                            *reinterpret_cast<float4 *>(to + y * (D / 8) + e) =
+                                make_float4(acc[e][2 * x + y], acc[e + 1][2 * x + y], acc[e + 2][2 * x + y], acc[e + 3][2 * x + y]);
+                    if (c == 0) part_ml[(int64_t)slot * kArRows + r] = make_float2(m[x], sum_l[x]);
+                }
+            }
+        }
+        left -= steps;
+        if (left == 0 && tid == 0) {
+            // a tile that begins here and goes on: the CTAs behind that have the rest of its blocks
+            const int rest = at.blocks - steps;
+            const bool goes_on = first == 0 && rest > 0;
+            join[blockIdx.x] = goes_on ? make_int4(at.row0, at.head, at.tile * kArRows | min(rows - at.tile * kArRows, kArRows) << 26,
+                                                   1 + (rest + chunk - 1) / chunk)
+                                       : make_int4(0, 0, 0, 0);
+        }
+        for (int b = 0; b < steps; ++b) at.next(a);
+    }
+    ptx::cp_async_wait<0>();
+}
+
+// Puts the parts of tile (CTA blockIdx.x of the kernel above) together: a thread per row and four columns.
+template <int D>
+__global__ void __launch_bounds__(kArRows * D / 4)
+attend_join_kernel(const __grid_constant__ AttendArgs a, const float *__restrict__ part, const float2 *__restrict__ part_ml,
+                   const int4 *__restrict__ join)
+{
+    ptx::grid_dep_launch();
+    ptx::grid_dep_wait();
+    const int4 what = join[blockIdx.x];
+    const int r = threadIdx.x / (D / 4), col = threadIdx.x % (D / 4) * 4;
+    if (what.w == 0 || r >= (int)((uint32_t)what.z >> 26)) return;
+    float top = kAtNothing;
+    for (int p = 0; p < what.w; ++p) {
+        const int slot = 2 * (blockIdx.x + p) + (p == 0 ? 1 : 0);
+        top = fmaxf(top, part_ml[(int64_t)slot * kArRows + r].x);
+    }
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+    for (int p = 0; p < what.w; ++p) {
+        const int64_t at = (int64_t)(2 * (blockIdx.x + p) + (p == 0 ? 1 : 0)) * kArRows + r;
+        const float2 ml = part_ml[at];
+        const float4 x = *reinterpret_cast<const float4 *>(part + at * D + col);
+        const float k = ex2(ml.x - top);
+        l = fmaf(ml.y, k, l);
+        o.x = fmaf(x.x, k, o.x);
+        o.y = fmaf(x.y, k, o.y);
+        o.z = fmaf(x.z, k, o.z);
+        o.w = fmaf(x.w, k, o.w);
+    }
+    const int m = (what.z & 0x3ffffff) + r, j = m / a.group;
+    const int64_t row = (int64_t)(what.x + j) * a.q_heads + what.y * a.group + (m - j * a.group);
+    const float k = l == 0.f ? 0.f : 1.f / l;
+    uint2 w;
+    __nv_bfloat162 *h = reinterpret_cast<__nv_bfloat162 *>(&w);
+    h[0] = __floats2bfloat162_rn(o.x * k, o.y * k);
+    h[1] = __floats2bfloat162_rn(o.z * k, o.w * k);
+    *reinterpret_cast<uint2 *>(a.out + row * D + col) = w;
+    if (a.lse && col == 0) a.lse[row] = l == 0.f ? -INFINITY : (top + log2f(l)) * kAtLn2;
+}
+
+}  // namespace rtp

@@ -80,14 +80,14 @@ def cache_write(x, slots, codes, scales):
 
 
 def attend(q, offsets, lens, tables, cache, scale, causal):
-    """(out, lse, weight) per row and head, in float64; weight = sum_t softmax_t |v_t|, dots = max_t scale sum_d |q_d k_td|:
-    what errors are relative to.  Rows of no request are NaN in all of them."""
+    """(out, lse, weight, dots, least) per row and head, in float64; weight = sum_t softmax_t |v_t|, dots = max_t scale sum_d |q_d k_td|,
+    least = max_t (softmax_t vs_t) sum_t |vc_t|: what errors are relative to.  Rows of no request are NaN."""
     kc, vc, ks, vs = cache
     rows, heads, dim = q.shape
     group = heads // kc.shape[1]
     out = torch.full((rows, heads, dim), math.nan, dtype=torch.float64)
     lse = torch.full((rows, heads), math.nan, dtype=torch.float64)
-    weight, dots = torch.full_like(out, math.nan), torch.zeros_like(lse)
+    weight, least, dots = torch.full_like(out, math.nan), torch.full_like(out, math.nan), torch.zeros_like(lse)
     for i in range(len(lens)):
         n, L = int(offsets[i + 1] - offsets[i]), int(lens[i])
         ids = tables[i, :-(-L // kc.shape[2])].long()
@@ -105,7 +105,10 @@ def attend(q, offsets, lens, tables, cache, scale, causal):
             # 0 * NaN of a block that a row does not see must not reach it
             out[r, h] = torch.stack([p[j, seen[j]] @ v[seen[j]] for j in range(n)]) if n else out[r, h]
             weight[r, h] = p @ v.abs().nan_to_num()
+            by = vs[ids, g].double().nan_to_num().repeat_interleave(kc.shape[2])[:L]
+            code = vc[ids, g].double().abs().reshape(-1, dim)[:L]
+            least[r, h] = (p * by).amax(-1, keepdim=True) * (seen.double() @ code) if L else 0.0
             lse[r, h] = z
             if L:
                 dots[r, h] = (x.abs() @ k.abs().T * abs(scale)).amax(-1)
-    return out, lse, weight, dots
+    return out, lse, weight, dots, least

@@ -128,7 +128,7 @@ def test_reference_attention_is_the_mean_for_equal_scores():
     cache.v.random_(-127, 128)
     cache.v_scale.fill_(0.5)
     q = torch.zeros(3, 1, 64)
-    out, lse, _, _ = ref.attend(q, [0, 3], [20], torch.tensor([[1, 0]]), cache, 1.0, True)
+    out, lse, _, _, _ = ref.attend(q, [0, 3], [20], torch.tensor([[1, 0]]), cache, 1.0, True)
     v = cache.v[[1, 0], 0].double().reshape(-1, 64) * 0.5
     for j in range(3):
         assert torch.allclose(out[j, 0], v[:18 + j].mean(0)) and abs(lse[j, 0] - math.log(18 + j)) < 1e-12

@@ -5,7 +5,10 @@ unit: 2^-8 of the value in bf16, 2^-24 in fp32) and fp32 arithmetic: the sum of 
 root, quotient, weight, cosine and sine (an angle off by 2^-24 of a turn = 4e-7), two products: under 2e-5 of the two elements that a rotation mixes
 in every case.  Attention: the output's rounding, 2^-8 of the value; a softmax weight is rounded to fp16 (2^-11 of it) and a
 score is an fp32 sum of D products, off by at most D 2^-24 of sum |q_d k_td| (128: 2^-17), which moves a weight by that factor;
-the sums of weights and products round in fp32 behind that (lengths up to 10^5: 2^-11 more, hardly ever that much).
+the sums of weights and products round in fp32 behind that (lengths up to 10^5: 2^-11 more, hardly ever that much).  A weight
+times its block's scale that is under 2^-14 of the row's largest is a subnormal number of fp16, whose steps are 2^-24 of that
+largest at most: off by 2^-25 of it, whatever its own size, for each token, times the token's code.  (It shows where one token has
+the whole softmax and a code of 0: the element is then the sum of the others' 2^-30ths.)
 """
 import math
 
@@ -232,15 +235,15 @@ def _check_attend(q, offsets, lens, tables, cache, max_q, max_len, scale=None, c
     binding.cache_attend(q, offsets, lens, tables, cache, max_q_len=max_q, max_seq_len=max_len, scale=scale, causal=causal, out=out,
                          lse=lse, **kw)
     dim = q.shape[2]
-    want, wlse, weight, dots = ref.attend(q.cpu(), offsets.tolist(), lens.tolist(), tables.cpu(), [t.cpu() for t in cache],
+    want, wlse, weight, dots, least = ref.attend(q.cpu(), offsets.tolist(), lens.tolist(), tables.cpu(), [t.cpu() for t in cache],
                                           dim ** -0.5 if scale is None else scale, causal)
     n = int(offsets[-1])
     got, glse = out.cpu().double(), lse.cpu().double()
     assert (got[n:] == keep).all() and (glse[n:] == keep).all()
-    want, wlse, weight, dots = want[:n], wlse[:n], weight[:n], dots[:n]
+    want, wlse, weight, dots, least = want[:n], wlse[:n], weight[:n], dots[:n], least[:n]
     err = (2.0 ** -17 * dots)[..., None]
     off = (got[:n] - want).abs()
-    bound = 2.0 ** -8 * want.abs() + (2.0 ** -10 + 2 * err) * weight + 1e-30
+    bound = 2.0 ** -8 * want.abs() + (2.0 ** -10 + 2 * err) * weight + 2.0 ** -25 * least + 1e-30
     assert (off <= bound).all(), (off / bound).max()
     empty = torch.isinf(wlse)
     assert torch.equal(glse[:n][empty], wlse[empty])
