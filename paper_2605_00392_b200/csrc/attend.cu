@@ -5,51 +5,9 @@
 
 #include "attend.cuh"
 #include "attend_rows.cuh"
+#include "attend_tiles.cuh"
 
 namespace rtp {
-
-constexpr int kAtWarps = 4;
-
-// A warp per (row, head), one token after the other.
-__global__ void __launch_bounds__(32 * kAtWarps)
-attend_simple_kernel(const __grid_constant__ AttendArgs a)
-{
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per = a.c.dim / 32;
-    const int i = blockIdx.z, head = blockIdx.y, j = (int)blockIdx.x * kAtWarps + warp;
-    ptx::grid_dep_launch();
-    ptx::grid_dep_wait();
-    int row0, n, len;
-    if (!attend_request(a, i, row0, n, len) || j >= n) return;
-    const int64_t row = row0 + j;
-    const __nv_bfloat16 *qp = a.q + row * a.q_stride + (int64_t)head * a.c.dim + lane * per;
-    float q[4] = {}, acc[4] = {}, m = -INFINITY, l = 0.f;
-    for (int e = 0; e < per; ++e) q[e] = __bfloat162float(qp[e]) * a.scale_log2;
-    const int end = len < 0 ? 0 : a.causal ? min(len, len - n + j + 1) : len;
-    const int kvh = head / a.group;
-    bool nan = len < 0;
-    for (int t = 0; t < end; ++t) {
-        const int page = attend_page(a, i, t);
-        if (page < 0) {
-            nan = true;
-            break;
-        }
-        const int64_t block = (int64_t)page * a.c.kv_heads + kvh;
-        const int64_t at = (block * a.c.page_size + (t & (a.c.page_size - 1))) * a.c.dim + lane * per;
-        float s = 0.f;
-        for (int e = 0; e < per; ++e) s += q[e] * (float)a.c.k[at + e];
-        s = warp_sum(s) * __ldg(a.c.k_scale + block);
-        const float top = max_nan(m, s), keep = exp2f(m - top), p = exp2f(s - top);
-        l = l * keep + p;
-        const float pv = p * __ldg(a.c.v_scale + block);
-        for (int e = 0; e < per; ++e) acc[e] = acc[e] * keep + pv * (float)a.c.v[at + e];
-        m = top;
-    }
-    const float inv = nan ? __uint_as_float(0x7fc00000u) : end > 0 ? 1.f / l : 0.f;
-    __nv_bfloat16 *o = a.out + (row * a.q_heads + head) * a.c.dim + lane * per;
-    for (int e = 0; e < per; ++e) o[e] = __float2bfloat16_rn(acc[e] * inv);
-    if (a.lse && lane == 0)
-        a.lse[row * a.q_heads + head] = nan ? inv : end > 0 ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
-}
 
 constexpr int kAtFewRows = 64;               // rows of a kv head up to which attend_rows_kernel takes the call
 
@@ -99,6 +57,19 @@ static cudaError_t launch_rows(const AttendArgs &a, int ctas, uint8_t *ws, cudaS
                           (const float2 *)(ws + w.part_ml), (const int4 *)(ws + w.join));
 }
 
+template <int D>
+static cudaError_t launch_tiles(const AttendArgs &a, cudaStream_t st)
+{
+    static std::atomic<unsigned long long> ready{0};
+    const cudaError_t e = allow_smem(attend_tiles_kernel<D>, TlShape<D>::kSmem, ready);
+    if (e != cudaSuccess) return e;
+    // (a request has no more rows than there are)
+    const int64_t row_blocks = ((int64_t)std::min(a.max_q_len, a.rows) * a.group + kTlSoft - 1) / kTlSoft;
+    const int64_t ctas = row_blocks * a.batch * a.c.kv_heads;
+    if (ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
+    return launch_chained(attend_tiles_kernel<D>, dim3((unsigned)ctas), dim3(kTlThreads), (size_t)TlShape<D>::kSmem, st, a, (int)row_blocks);
+}
+
 }  // namespace rtp
 
 extern "C" rtprune_status_t rtprune_cache_attend_workspace(int32_t batch, int32_t max_q_len, int64_t max_seq_len, int32_t q_heads,
@@ -126,7 +97,9 @@ extern "C" rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *
         return RTPRUNE_ERR_INVALID_ARG;
     if (!cache_view(cache, c, status)) return status;
     if (q_heads % c.kv_heads || max_seq_len > (int64_t)max_pages * c.page_size) return RTPRUNE_ERR_INVALID_ARG;
-    if (rows > INT32_MAX || max_seq_len > INT32_MAX / 2 || batch > 65535 || q_heads > 4096) return RTPRUNE_ERR_UNSUPPORTED;
+    if (rows > INT32_MAX || max_seq_len > INT32_MAX / 2 || batch > 65535 || q_heads > 4096 ||
+        std::min<int64_t>(rows, max_q_len) * q_heads > INT32_MAX / 2)
+        return RTPRUNE_ERR_UNSUPPORTED;
     if (rows == 0 || batch == 0 || max_q_len == 0) return RTPRUNE_OK;
     if (!q || !offsets || !seq_lens || (!block_tables && max_pages) || !out || q_stride < (int64_t)q_heads * c.dim || q_stride % 8 ||
         (((uintptr_t)q | (uintptr_t)out) & 15u))
@@ -147,8 +120,8 @@ extern "C" rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *
         if (e != cudaSuccess) return RTPRUNE_ERR_CUDA;
         return cudaGetLastError() == cudaSuccess ? RTPRUNE_OK : RTPRUNE_ERR_CUDA;
     }
-    const dim3 grid((unsigned)((max_q_len + kAtWarps - 1) / kAtWarps), (unsigned)q_heads, (unsigned)batch);
-    if (launch_chained(attend_simple_kernel, grid, dim3(32 * kAtWarps), (size_t)0, (cudaStream_t)cuda_stream, a) != cudaSuccess)
+    const cudaError_t e = c.dim == 128 ? launch_tiles<128>(a, (cudaStream_t)cuda_stream) : launch_tiles<64>(a, (cudaStream_t)cuda_stream);
+    if (e != cudaSuccess)
         return RTPRUNE_ERR_CUDA;
     return cudaGetLastError() == cudaSuccess ? RTPRUNE_OK : RTPRUNE_ERR_CUDA;
 }
