@@ -417,7 +417,7 @@ rtprune_status_t rtprune_cache_write(void *cuda_stream, rtprune_dtype_t dtype, c
  *   max_q_len, max_seq_len  HOST upper bounds of n_i and L_i, max_seq_len <= max_pages * page_size; they choose the kernels and the
  *                grid, not the result
  *   block_tables DEVICE int32 [batch] rows, table_stride apart, of max_pages entries
- *   out          DEVICE bf16 [rows][q_heads][head_dim], 16-byte aligned; lse DEVICE float [rows][q_heads], may be NULL.
+ *   out          DEVICE bf16 [rows][q_heads][head_dim], 32-byte aligned; lse DEVICE float [rows][q_heads], may be NULL.
  *                Rows of no request are left as they are.
  *   workspace    DEVICE, 256-byte aligned, of what rtprune_cache_attend_workspace says for the same sizes; its contents do not
  *                matter and it serves one call at a time

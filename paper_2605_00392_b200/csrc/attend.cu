@@ -11,6 +11,9 @@ namespace rtp {
 
 constexpr int kAtFewRows = 64;               // rows of a kv head up to which attend_rows_kernel takes the call
 
+// Whether attend_rows_kernel takes the call: few rows, or more heads of a kv head than a tile has rows.
+static bool few_rows(int64_t max_q_len, int group) { return max_q_len * group <= kAtFewRows || group > kTlRows; }
+
 // Workspace of attend_rows_kernel with `ctas` CTAs.
 struct RowsLayout {
     size_t part, part_ml, join, total;
@@ -57,17 +60,48 @@ static cudaError_t launch_rows(const AttendArgs &a, int ctas, uint8_t *ws, cudaS
                           (const float2 *)(ws + w.part_ml), (const int4 *)(ws + w.join));
 }
 
+// Items of the longest request that the call can have (it has no more rows than there are).
+static int64_t tile_row_blocks(const AttendArgs &a)
+{
+    const int tokens = kTlTiles * (kTlRows / a.group);
+    return (std::min(a.max_q_len, a.rows) + tokens - 1) / tokens;
+}
+
+// The queries as a tensor (element, head, row); boxes of 64 elements of `heads` heads of `tokens` rows, 128-byte swizzle.
+static bool queries_map(CUtensorMap *map, const AttendArgs &a, int heads, int tokens)
+{
+    typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                      const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                      CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static std::atomic<void *> encode{nullptr};       // the driver's entry point, looked up once
+    void *fn = encode.load(std::memory_order_relaxed);
+    if (!fn) {
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            return false;
+        encode.store(fn, std::memory_order_relaxed);
+    }
+    const cuuint64_t dims[3] = {(cuuint64_t)a.c.dim, (cuuint64_t)a.q_heads, (cuuint64_t)a.rows};
+    const cuuint64_t strides[2] = {(cuuint64_t)a.c.dim * 2, (cuuint64_t)a.q_stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)heads, (cuuint32_t)tokens}, unit[3] = {1, 1, 1};
+    return ((EncodeTiledFn)fn)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16 *>(a.q), dims, strides, box, unit,
+                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D>
 static cudaError_t launch_tiles(const AttendArgs &a, cudaStream_t st)
 {
     static std::atomic<unsigned long long> ready{0};
     const cudaError_t e = allow_smem(attend_tiles_kernel<D>, TlShape<D>::kSmem, ready);
     if (e != cudaSuccess) return e;
-    // (a request has no more rows than there are)
-    const int64_t row_blocks = ((int64_t)std::min(a.max_q_len, a.rows) * a.group + kTlSoft - 1) / kTlSoft;
-    const int64_t ctas = row_blocks * a.batch * a.c.kv_heads;
-    if (ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
-    return launch_chained(attend_tiles_kernel<D>, dim3((unsigned)ctas), dim3(kTlThreads), (size_t)TlShape<D>::kSmem, st, a, (int)row_blocks);
+    const int sms = device_sms(), tokens = kTlRows / a.group;
+    CUtensorMap map;
+    if (!sms || !queries_map(&map, a, a.group, tokens)) return cudaErrorUnknown;
+    const int64_t blocks = tile_row_blocks(a), items = blocks * a.batch * a.c.kv_heads;
+    return launch_chained(attend_tiles_kernel<D>, dim3((unsigned)std::min<int64_t>(items, sms)), dim3(kTlThreads), (size_t)TlShape<D>::kSmem, st,
+                          a, map, (int)blocks, tokens);
 }
 
 }  // namespace rtp
@@ -78,7 +112,7 @@ extern "C" rtprune_status_t rtprune_cache_attend_workspace(int32_t batch, int32_
     if (!workspace_bytes || batch < 0 || max_q_len < 0 || max_seq_len < 0 || q_heads <= 0 || kv_heads <= 0 || head_dim <= 0)
         return RTPRUNE_ERR_INVALID_ARG;
     *workspace_bytes = 256;
-    if ((int64_t)max_q_len * (q_heads / kv_heads) <= rtp::kAtFewRows)
+    if (rtp::few_rows(max_q_len, q_heads / kv_heads))
         *workspace_bytes = rtp::rows_layout(rtp::kArMostCtas, head_dim).total;
     return RTPRUNE_OK;
 }
@@ -97,12 +131,12 @@ extern "C" rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *
         return RTPRUNE_ERR_INVALID_ARG;
     if (!cache_view(cache, c, status)) return status;
     if (q_heads % c.kv_heads || max_seq_len > (int64_t)max_pages * c.page_size) return RTPRUNE_ERR_INVALID_ARG;
-    if (rows > INT32_MAX || max_seq_len > INT32_MAX / 2 || batch > 65535 || q_heads > 4096 ||
-        std::min<int64_t>(rows, max_q_len) * q_heads > INT32_MAX / 2)
+    if (rows > INT32_MAX / 2 || max_seq_len > INT32_MAX / 2 || batch > 65535 || q_heads > 4096 ||
+        rows * q_heads > INT32_MAX)
         return RTPRUNE_ERR_UNSUPPORTED;
     if (rows == 0 || batch == 0 || max_q_len == 0) return RTPRUNE_OK;
     if (!q || !offsets || !seq_lens || (!block_tables && max_pages) || !out || q_stride < (int64_t)q_heads * c.dim || q_stride % 8 ||
-        (((uintptr_t)q | (uintptr_t)out) & 15u))
+        ((uintptr_t)q & 15u) || ((uintptr_t)out & 31u))
         return RTPRUNE_ERR_INVALID_ARG;
     size_t need = 0;
     status = rtprune_cache_attend_workspace(batch, max_q_len, max_seq_len, q_heads, c.kv_heads, c.dim, &need);
@@ -111,7 +145,7 @@ extern "C" rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *
     AttendArgs a = {(const __nv_bfloat16 *)q, q_stride, offsets, seq_lens, block_tables, table_stride, batch, (int)rows, q_heads,
                     q_heads / c.kv_heads, max_q_len, (int)max_seq_len, max_pages, c, scale * 1.4426950408889634f, causal ? 1 : 0,
                     (__nv_bfloat16 *)out, lse};
-    if ((int64_t)max_q_len * a.group <= kAtFewRows) {
+    if (few_rows(max_q_len, a.group)) {
         const int ctas = std::min(kArPerSm * device_sms(), kArMostCtas);
         if (!ctas) return RTPRUNE_ERR_CUDA;
         uint8_t *ws = (uint8_t *)workspace;
@@ -120,6 +154,7 @@ extern "C" rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *
         if (e != cudaSuccess) return RTPRUNE_ERR_CUDA;
         return cudaGetLastError() == cudaSuccess ? RTPRUNE_OK : RTPRUNE_ERR_CUDA;
     }
+    if (tile_row_blocks(a) * batch * c.kv_heads > INT32_MAX / 2) return RTPRUNE_ERR_UNSUPPORTED;
     const cudaError_t e = c.dim == 128 ? launch_tiles<128>(a, (cudaStream_t)cuda_stream) : launch_tiles<64>(a, (cudaStream_t)cuda_stream);
     if (e != cudaSuccess)
         return RTPRUNE_ERR_CUDA;

@@ -1,14 +1,18 @@
 // Attention of many query rows per kv head (prefill) over the 8-bit paged cache, on the tcgen05 tensor cores.
 //
-// A CTA takes 256 rows (token by token, a token's heads of one kv head beside each other) of a request and kv head as two tiles of
-// 128, against blocks of 128 tokens:
+// A CTA takes two tiles of rows of a request and kv head, each as many tokens as fit 128 rows with all their heads of that kv
+// head (a row per token and head, a token's heads beside each other), against blocks of 128 cached tokens:
 //   S = Q K^T   fp16 operands in shared memory, fp32 sums in TMEM
 //   P           fp16 weights, written over S in TMEM by the thread that owns the row
 //   O += P V    P from TMEM, V from shared memory, fp32 sums in TMEM
-// Warps 0-3 and 4-7: a row per thread of the first and second tile (queries in, softmax, output).  Warps 8-11 take the codes of a block
-// from global memory to fp16 in the swizzled operand layout; both operands are tiles of (token, 64 elements), K-major for the keys,
-// MN-major for the values.  Warp 12 issues the MMAs.  While one tile's softmax runs, the other's MMAs do; S of a tile's next block is
-// issued behind the PV of this one, whose P it overwrites.
+// One CTA per SM takes items (two tiles) blockIdx.x, + gridDim.x, ...; what its warps do:
+//   0-3, 4-7  a row per thread of the first and second tile: softmax, output; and the next item's queries from bf16 to fp16, in place
+//   8-11      codes to fp16 in the swizzled operand layout (tiles of (token, 64 elements), K-major for the keys, MN-major for the values)
+//   12        issues the MMAs    13  finds the items    14  bulk copies of codes    15  the queries, by TMA
+// While one tile's softmax runs, the other's MMAs do; S of a tile's next block is issued behind the PV of this one, whose P it
+// overwrites.  One item's output leaves while the next one's scores are computed.
+// Everything large comes by bulk copies: with 227 KB of shared memory there are some 20 KB of L1 left, and ordinary loads of
+// 64 KB of queries, which need a line of it each while they are on their way, took 10,000 cycles.
 // A row's sums are rescaled only when its maximum has grown by more than 2^8 (the weights have that room in fp16).
 // Bound by the tensor cores and, about as much, by the exponentials: 128 x 128 scores take 1024 cycles of either (16 exponentials a
 // cycle and SM; two products of 128^3 at 4096 multiply-adds).
@@ -21,9 +25,9 @@ constexpr int kTlRows = 128;                         // rows of a tile
 constexpr int kTlTiles = 2;
 constexpr int kTlBlock = 128;                        // tokens of a block
 constexpr int kTlSoft = kTlTiles * kTlRows;
-constexpr int kTlThreads = kTlSoft + 128 + 128;     // (three of the last four warps only give up their registers)
-constexpr int kTlSoftRegs = 176, kTlCodeRegs = 112, kTlMmaRegs = 48;   // registers of a thread by role: 2, 1, 1 of four warpgroups at 128
-static_assert(2 * kTlSoftRegs + kTlCodeRegs + kTlMmaRegs <= 4 * 128, "what the block was launched with");
+constexpr int kTlThreads = kTlSoft + 128 + 128;     // (the last warp only makes it 128 registers a thread)
+constexpr int kTlSoftRegs = 168, kTlCodeRegs = 88, kTlOtherRegs = 88;    // registers of a thread: 2, 1, 1 of four warpgroups
+static_assert(2 * kTlSoftRegs + kTlCodeRegs + kTlOtherRegs <= 4 * 128, "what the block was launched with");
 constexpr int kTlGroups = kTlBlock / 16;             // a page holds at least 16 tokens: scales are per 16
 
 constexpr float kTlLarge = 1048576.f;                // scores under this are rounded by less than 2^-4
@@ -31,16 +35,42 @@ constexpr float kTlLarge = 1048576.f;                // scores under this are ro
 template <int D> struct TlShape {
     static constexpr int kSlabs = D / 64;
     static constexpr int kSlab = 128 * 128;          // 128 rows (tokens) of 64 fp16
-    static constexpr int kOperand = kSlabs * kSlab;
-    static constexpr int kSmem = (kTlTiles + 4) * kOperand + 1024 /*alignment*/ + 1024 /*scales, barriers*/;
+    static constexpr int kOperand = kSlabs * kSlab;  // queries of a tile; keys or values of a block
+    static constexpr int kSlot = kTlBlock * D;       // codes of a block
+    static constexpr int kSlots = D == 128 ? 2 : 4;
+    static constexpr int kSmem = (kTlTiles + 4) * kOperand + kSlots * kSlot + 1024 /*alignment*/;
 };
 
+// A CTA's piece of work.
+struct TlItem {
+    int i, head, j0, row0, n, len;                   // i < 0: no more; j0: first of its tokens, in the request
+    int blocks[kTlTiles];                            // blocks of tokens that each tile sees any of
+};
+constexpr int kTlItems = 4;                          // pieces that the scheduler may be ahead by, about
+constexpr int kTlReaders = 15;                       // warps that read them
+constexpr int kTlGroupRing = 8;
+
 struct TlShared {
-    float4 group[4][kTlGroups];                      // ks, log2 vs, 1 / vs of each 16 tokens of block j at j mod 4
-    uint64_t q_full, k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[kTlTiles], p_full[kTlTiles], o_full;
+    float4 group[kTlGroupRing][kTlGroups];           // ks, log2 vs, 1 / vs of each 16 tokens of the line's n-th block at n mod kTlGroupRing
+    TlItem item[kTlItems];
+    uint64_t item_full[kTlItems], item_empty[kTlItems];
+    uint64_t code_full[4], code_empty[4];            // keys of block 0, values of block 0, keys of block 1, ...
+    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
+    uint64_t q_raw[kTlTiles], q_full[kTlTiles], q_empty[kTlTiles], s_full[kTlTiles], p_full[kTlTiles], o_full[kTlTiles], o_empty[kTlTiles];
+    uint64_t done;
     uint32_t tmem;
     volatile int gave_up;
 };
+
+// The k-th item, for a whole warp.  false: a wait gave up.
+__device__ inline bool tl_take(TlShared *sh, uint32_t k, TlItem &t)
+{
+    const bool ok = ptx::mbar_wait(&sh->item_full[k % kTlItems], k / kTlItems & 1);
+    t = sh->item[k % kTlItems];
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&sh->item_empty[k % kTlItems]);
+    return __all_sync(0xffffffffu, ok);
+}
 
 __device__ inline void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
 {
@@ -59,6 +89,13 @@ __device__ inline void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
         "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
+// One lane of a full warp, the same each time.
+__device__ inline bool elect_one()
+{
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
 __device__ inline void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // Instruction descriptor of kind::f16 with fp16 operands (see ptx::idesc_bf16).
 __device__ inline uint32_t idesc_f16(int M, int N, bool b_mn_major)
@@ -68,7 +105,25 @@ __device__ inline uint32_t idesc_f16(int M, int N, bool b_mn_major)
 
 template <int N> __device__ inline void regs_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ inline void regs_fewer() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-
+// 32 bytes, a whole sector of one lane's row (32-byte aligned).
+__device__ inline void st_global_v8(void *p, const uint32_t *v)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
+                 "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+__device__ inline uint4 ld_shared_u4(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ inline uint32_t max2_nan(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 // Two fp32 at a time.
 __device__ inline uint64_t pack2(float a, float b)
 {
@@ -90,43 +145,93 @@ __device__ inline uint64_t add2(uint64_t a, uint64_t b)
     return r;
 }
 
-// Weights of a row's 128 scores `v` in its place in TMEM, their sum (without the values' scale) into l.  kCare: tokens from `left` on are not
-// seen, and scores may be so large that their own rounding matters, which the maximum went through: they go through it too before
-// the maximum is taken off.
-template <bool kCare>
-__device__ inline void tile_weights(const uint32_t (&v)[kTlBlock], const float4 *group, float factor, float top, int left, uint32_t t_s, float &l)
+__device__ inline float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }    // (one instruction)
+__device__ inline float max16(const float (&s)[16])
+{
+    const float a = max3(s[0], s[1], s[2]), b = max3(s[3], s[4], s[5]), c = max3(s[6], s[7], s[8]), d = max3(s[9], s[10], s[11]);
+    return max3(max3(a, b, c), max3(d, s[12], s[13]), fmaxf(s[14], s[15]));
+}
+
+// The largest s' of 32 of a row's scores (two groups), and their weights to the place `to` in TMEM, the sum of these (without the values'
+// scale) into l.  The scores come from TMEM once for each, 32 at a time: a thread that keeps its 128 spills whatever else it has,
+// and what is spilled comes back from L2 (shared memory has left L1 next to nothing).
+__device__ inline float tile_top(const uint32_t (&v)[32], const float4 *group, float factor, float now)
 {
 #pragma unroll
-    for (int c = 0; c < kTlBlock / 32; ++c) {
-        uint32_t p[16];
+    for (int h = 0; h < 2; ++h) {
+        float s[16];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int e = 0; e < 16; ++e) s[e] = __uint_as_float(v[16 * h + e]);
+        const float4 g = group[h];
+        now = fmaxf(now, fmaf(max16(s), factor * g.x, g.y));
+    }
+    return now;
+}
+__device__ inline void tile_weights(const uint32_t (&v)[32], const float4 *group, float factor, float top, uint32_t to, float &l)
+{
+    uint32_t p[16];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const float4 g = group[h];
+        const float k = factor * g.x, b = g.y - top;
+        const uint64_t k2 = pack2(k, k), b2 = pack2(b, b);
+        uint64_t sum2 = 0;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            float w0, w1;
+            unpack2(fma2(pack2(__uint_as_float(v[16 * h + e]), __uint_as_float(v[16 * h + e + 1])), k2, b2), w0, w1);
+            w0 = ex2(w0);
+            w1 = ex2(w1);
+            sum2 = add2(sum2, pack2(w0, w1));
+            p[8 * h + e / 2] = pack_half(w0, w1);
+        }
+        float s0, s1;
+        unpack2(sum2, s0, s1);
+        l = fmaf(s0 + s1, g.z, l);
+    }
+    tmem_st16(to, p);
+}
+// The same where tokens from `left` on are not seen, or scores are so large that their own rounding matters: it is what the maximum
+// went through, so they go through it too before the maximum is taken off.  Loops of few instructions, from TMEM again.
+__device__ inline float careful_top(const float4 *group, float factor, int left, uint32_t t_s)
+{
+    float now = kAtNothing;
+#pragma unroll 1
+    for (int c = 0; c < kTlGroups; ++c, left -= 16) {
+        uint32_t v[16];
+        ptx::tmem_ld16(t_s + c * 16, v);
+        ptx::tmem_ld_wait();
+        float s[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = e < left ? __uint_as_float(v[e]) : -INFINITY;
+        const float4 g = group[c];
+        now = fmaxf(now, fmaf(max16(s), factor * g.x, g.y));
+    }
+    return now;
+}
+__device__ inline void careful_weights(const float4 *group, float factor, float top, int left, uint32_t t_s, float &l)
+{
+#pragma unroll 1
+    for (int c = 0; c < kTlBlock / 32; ++c) {
+        uint32_t v[32], p[16];
+        ptx::tmem_ld32(t_s + c * 32, v);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int h = 0; h < 2; ++h, left -= 16) {
             const float4 g = group[2 * c + h];
-            const float k = factor * g.x, b = kCare ? g.y : g.y - top;
-            const uint64_t k2 = pack2(k, k), b2 = pack2(b, b);
-            uint64_t sum2 = 0;
+            const float k = factor * g.x;
+            float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-                const int at = 32 * c + 16 * h + e;
-                float w0, w1;
-                unpack2(fma2(pack2(__uint_as_float(v[at]), __uint_as_float(v[at + 1])), k2, b2), w0, w1);
-                if (kCare) {
-                    w0 -= top;
-                    w1 -= top;
-                }
-                w0 = ex2(w0);
-                w1 = ex2(w1);
-                if (kCare) {
-                    if (at >= left) w0 = 0.f;
-                    if (at + 1 >= left) w1 = 0.f;
-                }
-                sum2 = add2(sum2, pack2(w0, w1));
+                float w0 = ex2(fmaf(__uint_as_float(v[16 * h + e]), k, g.y) - top);
+                float w1 = ex2(fmaf(__uint_as_float(v[16 * h + e + 1]), k, g.y) - top);
+                w0 = e < left ? w0 : 0.f;
+                w1 = e + 1 < left ? w1 : 0.f;
+                sum += w0 + w1;
                 p[8 * h + e / 2] = pack_half(w0, w1);
             }
-            float s0, s1;
-            unpack2(sum2, s0, s1);
             // weights of 0 add nothing, whatever the block's scale is (of a page that the row does not see)
-            if (!kCare || s0 + s1 != 0.f) l = fmaf(s0 + s1, g.z, l);
+            if (sum != 0.f) l = fmaf(sum, g.z, l);
         }
         tmem_st16(t_s + c * 16, p);
     }
@@ -134,49 +239,43 @@ __device__ inline void tile_weights(const uint32_t (&v)[kTlBlock], const float4 
 
 template <int D>
 __global__ void __launch_bounds__(kTlThreads, 1)
-attend_tiles_kernel(const __grid_constant__ AttendArgs a, int row_blocks)
+attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map_q, int row_blocks, int tile_tokens)
 {
     using S = TlShape<D>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    TlShared *sh = reinterpret_cast<TlShared *>(smem + (kTlTiles + 4) * S::kOperand);
-    static_assert(sizeof(TlShared) <= 1024, "");
+    __shared__ TlShared shared;
+    TlShared *const sh = &shared;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    ptx::grid_dep_launch();
-    ptx::grid_dep_wait();
-    // the last rows of every request first: with a causal mask they have the most to do
-    const int per = a.batch * a.c.kv_heads, rb = row_blocks - 1 - (int)blockIdx.x / per, rest = (int)blockIdx.x % per;
-    const int i = rest / a.c.kv_heads, head = rest % a.c.kv_heads;
-    int row0, n, len;
-    if (!attend_request(a, i, row0, n, len)) return;
-    const int rows = n * a.group, m0 = rb * kTlSoft;
-    if (m0 >= rows) return;
-    // blocks of tokens that each tile sees any of
-    int blocks[kTlTiles];
-#pragma unroll
-    for (int x = 0; x < kTlTiles; ++x) {
-        const int first = m0 + x * kTlRows, last = min(first + kTlRows, rows) - 1;
-        const int end = first >= rows || len < 0 ? 0 : a.causal ? min(len, len - n + 1 + last / a.group) : len;
-        blocks[x] = (max(end, 0) + kTlBlock - 1) / kTlBlock;
-    }
-    const int most = max(blocks[0], blocks[1]);
-
     if (tid == 0) {
-        ptx::mbar_init(&sh->q_full, kTlSoft);
+        for (int s = 0; s < kTlItems; ++s) {
+            ptx::mbar_init(&sh->item_full[s], 1);
+            ptx::mbar_init(&sh->item_empty[s], kTlReaders);
+        }
+        for (int s = 0; s < S::kSlots; ++s) {
+            ptx::mbar_init(&sh->code_full[s], 1);
+            ptx::mbar_init(&sh->code_empty[s], 128);
+        }
         for (int s = 0; s < 2; ++s) {
             ptx::mbar_init(&sh->k_full[s], 128);
-            ptx::mbar_init(&sh->v_full[s], 128);
             ptx::mbar_init(&sh->k_empty[s], 1);
+            ptx::mbar_init(&sh->v_full[s], 128);
             ptx::mbar_init(&sh->v_empty[s], 1);
         }
         for (int x = 0; x < kTlTiles; ++x) {
+            ptx::mbar_init(&sh->q_raw[x], 1);
+            ptx::mbar_init(&sh->q_full[x], kTlRows);
+            ptx::mbar_init(&sh->q_empty[x], 1);
             ptx::mbar_init(&sh->s_full[x], 1);
             ptx::mbar_init(&sh->p_full[x], kTlRows);
+            ptx::mbar_init(&sh->o_full[x], 1);
+            ptx::mbar_init(&sh->o_empty[x], kTlRows);
         }
-        ptx::mbar_init(&sh->o_full, 1);
+        ptx::mbar_init(&sh->done, 1);
         sh->gave_up = 0;
         ptx::fence_mbar_init();
     }
+    ptx::grid_dep_wait();                            // (before TMEM is taken: a kernel ahead may be waiting for it)
     if (warp == 12) {
         ptx::tmem_alloc(&sh->tmem, 512);
         ptx::tmem_relinquish();
@@ -184,270 +283,447 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, int row_blocks)
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
-    const uint32_t tmem = sh->tmem, s_u32 = ptx::smem_u32(smem);
-    const uint32_t k_u32 = s_u32 + kTlTiles * S::kOperand, v_u32 = k_u32 + 2 * S::kOperand;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, sh->tmem, 0), s_u32 = ptx::smem_u32(smem);
+    const uint32_t k_u32 = s_u32 + kTlTiles * S::kOperand, v_u32 = k_u32 + 2 * S::kOperand, code_u32 = v_u32 + 2 * S::kOperand;
     // TMEM: scores (and weights over them) of the tiles at columns 0 and 128, outputs at 256 and 256 + D
+    // (not earlier: a kernel behind this one that takes TMEM before it waits could otherwise have it first)
+    ptx::grid_dep_launch();
 
-    if (warp >= 12) {
-        // ---------------- the MMAs ------------------------------------------------------------------------
-        regs_fewer<kTlMmaRegs>();
-        if (warp == 12 && lane == 0 && most > 0) {
-            const uint32_t id_s = idesc_f16(kTlRows, kTlBlock, false), id_o = idesc_f16(kTlRows, D, true);
-            bool ok = ptx::mbar_wait(&sh->q_full, 0) && ptx::mbar_wait(&sh->k_full[0], 0);
-            ptx::tc_fence_after();
-            auto scores = [&](int x, int s) {
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t at = (k >> 2) * S::kSlab + (k & 3) * 32;
-                    ptx::umma_bf16(tmem + x * 128, ptx::smem_desc_sw128(s_u32 + x * S::kOperand + at, 16, 1024),
-                                   ptx::smem_desc_sw128(k_u32 + s * S::kOperand + at, 16, 1024), id_s, k > 0);
+    // (each warpgroup by one instruction of its own)
+    if (warp >= 12) regs_fewer<kTlOtherRegs>();
+    else if (warp >= 8) regs_fewer<kTlCodeRegs>();
+    else regs_more<kTlSoftRegs>();
+    if (warp == 13) {
+        // ---------------- the work: items blockIdx.x, + gridDim.x, ... that have rows ------------------------
+        const int per = a.batch * a.c.kv_heads, all = row_blocks * per;
+        uint32_t k = 0;
+        int at = blockIdx.x;
+#pragma unroll 1
+        for (bool ok = true; ok; ++k) {
+            TlItem t;
+            t.i = -1;
+            // 32 of the numbers at a time, one per lane (bounds that are far above the requests' lengths leave most of them empty)
+#pragma unroll 1
+            for (; at < all; at += 32 * gridDim.x) {
+                const int mine = at + lane * gridDim.x;
+                bool has = false;
+                if (mine < all) {
+                    // the last rows of every request first: with a causal mask they have the most to do
+                    const int rest = mine % per;
+                    t.i = rest / a.c.kv_heads;
+                    t.head = rest - t.i * a.c.kv_heads;
+                    t.j0 = (row_blocks - 1 - mine / per) * kTlTiles * tile_tokens;
+                    has = attend_request(a, t.i, t.row0, t.n, t.len) && t.j0 < t.n;
                 }
-                ptx::umma_commit(&sh->s_full[x]);
-            };
-            if (ok) {
-                for (int x = 0; x < kTlTiles; ++x)
-                    if (blocks[x] > 0) scores(x, 0);
-                ptx::umma_commit(&sh->k_empty[0]);
-            }
-            for (int j = 0; ok && j < most; ++j) {
-                const int s = j & 1;
-                bool have_k = false, have_v = false;
-                for (int x = 0; ok && x < kTlTiles; ++x) {
-                    if (j >= blocks[x]) continue;
-                    ok = ptx::mbar_wait(&sh->p_full[x], s);
-                    if (ok && !have_v) ok = have_v = ptx::mbar_wait(&sh->v_full[s], (j >> 1) & 1);
-                    if (!ok) break;
-                    ptx::tc_fence_after();
-#pragma unroll
-                    for (int k = 0; k < kTlBlock / 16; ++k)
-                        umma_f16_ts(tmem + 256 + x * D, tmem + x * 128 + k * 8,
-                                    ptx::smem_desc_sw128(v_u32 + s * S::kOperand + k * 2048, S::kSlab, 1024), id_o, j > 0 || k > 0);
-                    if (j + 1 < blocks[x]) {
-                        if (!have_k) ok = have_k = ptx::mbar_wait(&sh->k_full[s ^ 1], ((j + 1) >> 1) & 1);
-                        if (!ok) break;
-                        ptx::tc_fence_after();
-                        scores(x, s ^ 1);
+                const uint32_t found = __ballot_sync(0xffffffffu, has);
+                if (found) {
+                    const int from = __ffs(found) - 1;
+                    at += (from + 1) * gridDim.x;
+                    if (lane == from) {
+#pragma unroll 1
+                        for (int x = 0; x < kTlTiles; ++x) {
+                            const int first = t.j0 + x * tile_tokens, last = min(first + tile_tokens, t.n) - 1;
+                            const int end = first >= t.n || t.len < 0 ? 0 : a.causal ? t.len - t.n + 1 + last : t.len;
+                            const int b = (max(end, 0) + kTlBlock - 1) / kTlBlock;
+                            if (x) t.blocks[1] = b;
+                            else t.blocks[0] = b;
+                        }
                     }
+                    t.i = __shfl_sync(0xffffffffu, t.i, from);
+                    t.head = __shfl_sync(0xffffffffu, t.head, from);
+                    t.j0 = __shfl_sync(0xffffffffu, t.j0, from);
+                    t.row0 = __shfl_sync(0xffffffffu, t.row0, from);
+                    t.n = __shfl_sync(0xffffffffu, t.n, from);
+                    t.len = __shfl_sync(0xffffffffu, t.len, from);
+                    t.blocks[0] = __shfl_sync(0xffffffffu, t.blocks[0], from);
+                    t.blocks[1] = __shfl_sync(0xffffffffu, t.blocks[1], from);
+                    break;
                 }
-                if (ok) {
-                    ptx::umma_commit(&sh->v_empty[s]);
-                    if (j + 1 < most) ptx::umma_commit(&sh->k_empty[s ^ 1]);
+                t.i = -1;
+            }
+            if (k >= kTlItems) ok = ptx::mbar_wait(&sh->item_empty[k % kTlItems], (k / kTlItems - 1) & 1);
+            if (ok && lane == 0) {
+                sh->item[k % kTlItems] = t;
+                ptx::mbar_arrive(&sh->item_full[k % kTlItems]);
+            }
+            if (!ok) sh->gave_up = 1;
+            if (t.i < 0) break;
+        }
+    } else if (warp == 14) {
+        // ---------------- codes of the items' blocks, and their scales ----------------------------------------
+        const int per_page = min(a.c.page_size, kTlBlock), copies = kTlBlock / per_page;   // a page of a head is one piece of memory
+        TlItem t;
+        bool ok = true;
+        uint32_t n = 0, copy = 0;                    // blocks, slots so far
+#pragma unroll 1
+        for (uint32_t item = 0; ok && (ok = tl_take(sh, item, t)) && t.i >= 0; ++item) {
+            const int most = max(t.blocks[0], t.blocks[1]);
+#pragma unroll 1
+            for (int j = 0; ok && j < most; ++j, ++n) {
+                // lane: a copy's page, and (lane < 8) the page of its 16 tokens.  Tokens behind the end are not fetched: what lies in
+                // the slot are codes too, and nobody sees them
+                const int t0 = j * kTlBlock, t_copy = t0 + lane * per_page, t_group = t0 + lane * 16;
+                const int page = lane < copies && t_copy < t.len ? attend_page(a, t.i, t_copy) : -1;
+                const int page_g = lane < kTlGroups && t_group < t.len ? attend_page(a, t.i, t_group) : -1;
+                if (lane < kTlGroups) {
+                    const int64_t block = (int64_t)max(page_g, 0) * a.c.kv_heads + t.head;
+                    const float nan = __uint_as_float(0x7fc00000u);
+                    float lv, inv;
+                    value_scale(page_g < 0 ? nan : __ldg(a.c.v_scale + block), lv, inv);
+                    sh->group[n % kTlGroupRing][lane] = make_float4(page_g < 0 ? nan : __ldg(a.c.k_scale + block), lv, inv, 0.f);
                 }
+                const uint32_t bytes = (uint32_t)(__popc(__ballot_sync(0xffffffffu, page >= 0)) * per_page * D);
+                const int64_t from = ((int64_t)max(page, 0) * a.c.kv_heads + t.head) * a.c.page_size * D;
+#pragma unroll 1
+                for (int v = 0; ok && v < 2; ++v, ++copy) {
+                    const uint32_t slot = copy % S::kSlots, turn = copy / S::kSlots;
+                    if (turn > 0) ok = ptx::mbar_wait(&sh->code_empty[slot], (turn - 1) & 1);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    if (lane == 0) ptx::mbar_arrive_expect_tx(&sh->code_full[slot], bytes);
+                    __syncwarp();
+                    if (page >= 0)
+                        ptx::bulk_load(code_u32 + slot * S::kSlot + lane * per_page * D, (v ? a.c.v : a.c.k) + from, (uint32_t)(per_page * D), &sh->code_full[slot]);
+                }
+            }
+        }
+        if (!ok) sh->gave_up = 1;
+        // no copy is left on its way into memory that this CTA gives back
+        for (uint32_t c = copy > S::kSlots ? copy - S::kSlots : 0; c < copy; ++c)
+            ptx::mbar_wait(&sh->code_full[c % S::kSlots], c / S::kSlots & 1);
+    } else if (warp == 15) {
+        // ---------------- the coming items' queries, as they are, in the operand's layout already ---------------
+        TlItem t;
+        bool ok = true;
+        uint32_t uses[kTlTiles] = {0, 0};
+#pragma unroll 1
+        for (uint32_t item = 0; ok && (ok = tl_take(sh, item, t)) && t.i >= 0; ++item) {
+#pragma unroll 1
+            for (int x = 0; ok && x < kTlTiles; ++x) {
+                if ((x ? t.blocks[1] : t.blocks[0]) == 0) continue;
+                const uint32_t before = x ? uses[1] : uses[0];
+                if (before > 0) ok = ptx::mbar_wait(&sh->q_empty[x], (before - 1) & 1);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (lane == 0) {
+                    ptx::mbar_arrive_expect_tx(&sh->q_raw[x], (uint32_t)(S::kSlabs * tile_tokens * a.group * 128));
+                    for (int b = 0; b < S::kSlabs; ++b)
+                        ptx::tma_load_3d(s_u32 + x * S::kOperand + b * S::kSlab, &map_q, &sh->q_raw[x], b * 64, t.head * a.group,
+                                         t.row0 + t.j0 + x * tile_tokens);
+                }
+                __syncwarp();
+                if (x) ++uses[1];
+                else ++uses[0];
+            }
+        }
+        if (!ok) sh->gave_up = 1;
+        for (int x = 0; x < kTlTiles; ++x)
+            if (uses[x] > 0) ptx::mbar_wait(&sh->q_raw[x], (uses[x] - 1) & 1);
+    } else if (warp >= 12) {
+        // ---------------- the MMAs ------------------------------------------------------------------------
+        // the whole warp walks the blocks, one elected lane issues; loops of few instructions (all roles' code together is what
+        // the instruction caches have to hold: unrolled and inlined freely it was 160 KB, and each item began with misses)
+        if (warp == 12) {
+            const bool issuer = elect_one();
+            const uint32_t id_s = idesc_f16(kTlRows, kTlBlock, false), id_o = idesc_f16(kTlRows, D, true);
+            // descriptors differ from these by multiples of 16 bytes in the address (their low 14 bits, which never carry)
+            const uint64_t d_q = ptx::smem_desc_sw128(s_u32, 16, 1024), d_k = ptx::smem_desc_sw128(k_u32, 16, 1024);
+            const uint64_t d_v = ptx::smem_desc_sw128(v_u32, S::kSlab, 1024);
+            bool ok = true;
+            uint32_t n = 0, items[kTlTiles] = {0, 0}, turns[kTlTiles] = {0, 0};     // blocks; each tile's items and blocks so far
+            TlItem t;
+#pragma unroll 1
+            for (uint32_t item = 0; ok && (ok = tl_take(sh, item, t)) && t.i >= 0; ++item) {
+                const int most = max(t.blocks[0], t.blocks[1]);
+                // step j: products of block j - 1 and scores of block j, tile by tile
+#pragma unroll 1
+                for (int j = 0; ok && most > 0 && j <= most; ++j, ++n) {
+                    // n: the line's number of block j
+                    bool have_k = false, have_v = false;
+#pragma unroll 1
+                    for (int x = 0; ok && x < kTlTiles; ++x) {
+                        const int mine = x ? t.blocks[1] : t.blocks[0];
+                        const uint32_t before = x ? items[1] : items[0], turn = x ? turns[1] : turns[0];
+                        if (j > 0 && j <= mine) {
+                            // the last item's output has been taken out of TMEM
+                            if (j == 1 && before > 0) ok = ptx::mbar_wait(&sh->o_empty[x], (before - 1) & 1);
+                            if (ok) ok = ptx::mbar_poll(&sh->p_full[x], turn & 1);
+                            if (ok && !have_v) ok = have_v = ptx::mbar_wait(&sh->v_full[(n - 1) & 1], ((n - 1) >> 1) & 1);
+                            if (!ok) break;
+                            ptx::tc_fence_after();
+                            if (issuer) {
+                                uint64_t v0 = d_v + ((n - 1) & 1) * (S::kOperand >> 4);
+                                uint32_t p0 = tmem + x * 128;
+#pragma unroll 1
+                                for (int k = 0; k < kTlBlock / 16; k += 4, v0 += 4 * 2048 >> 4, p0 += 32)
+#pragma unroll
+                                    for (int y = 0; y < 4; ++y)
+                                        umma_f16_ts(tmem + 256 + x * D, p0 + y * 8, v0 + y * (2048 >> 4), id_o, j - 1 + k + y > 0);
+                                if (j == mine) ptx::umma_commit(&sh->o_full[x]);
+                            }
+                            __syncwarp();
+                            if (x) ++turns[1];
+                            else ++turns[0];
+                        }
+                        if (j < mine) {
+                            if (j == 0) ok = ptx::mbar_wait(&sh->q_full[x], before & 1);
+                            if (ok && !have_k) ok = have_k = ptx::mbar_wait(&sh->k_full[n & 1], (n >> 1) & 1);
+                            if (!ok) break;
+                            ptx::tc_fence_after();
+                            if (issuer) {
+                                uint64_t q = d_q + x * (S::kOperand >> 4), k0 = d_k + (n & 1) * (S::kOperand >> 4);
+#pragma unroll 1
+                                for (int b = 0; b < S::kSlabs; ++b, q += S::kSlab >> 4, k0 += S::kSlab >> 4)
+#pragma unroll
+                                    for (int k = 0; k < 4; ++k) ptx::umma_bf16(tmem + x * 128, q + 2 * k, k0 + 2 * k, id_s, b + k > 0);
+                                ptx::umma_commit(&sh->s_full[x]);
+                                if (j + 1 == mine) ptx::umma_commit(&sh->q_empty[x]);
+                            }
+                            __syncwarp();
+                        }
+                    }
+                    if (ok && issuer) {
+                        if (j > 0) ptx::umma_commit(&sh->v_empty[(n - 1) & 1]);
+                        if (j < most) ptx::umma_commit(&sh->k_empty[n & 1]);
+                    }
+                    __syncwarp();
+                    if (j == most) break;            // (the next item's first block has this number)
+                }
+                items[0] += t.blocks[0] > 0;
+                items[1] += t.blocks[1] > 0;
             }
             if (!ok) sh->gave_up = 1;
             // all MMAs done (also after a wait that gave up: the memory they use is about to be freed)
-            ptx::umma_commit(&sh->o_full);
-            if (!ptx::mbar_wait(&sh->o_full, 0)) sh->gave_up = 1;
+            if (issuer) ptx::umma_commit(&sh->done);
+            __syncwarp();
+            if (!ptx::mbar_wait(&sh->done, 0)) sh->gave_up = 1;
         }
     } else if (warp >= 8) {
         // ---------------- codes to fp16 ---------------------------------------------------------------------
-        // a thread's pieces: 16 codes of token 32 w + 8 q + lane / 4, piece lane % 4 of each slab: eight neighbouring lanes then
-        // store to eight different places of a 128-byte line
-        regs_fewer<kTlCodeRegs>();
-        const int w = warp - 8, ct = tid - kTlSoft, r = lane >> 2, pc = lane & 3;
-        constexpr int kPieces = 4 * S::kSlabs;
-        auto page_of = [&](int j, int half) { return attend_page(a, i, min(j * kTlBlock + 32 * w + 16 * half, max(len - 1, 0))); };
-        auto load = [&](const int8_t *codes, int j, const int (&page)[2], uint4 (&x)[kPieces]) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int t = j * kTlBlock + 32 * w + 8 * q + r;
-                const int8_t *from = codes + (((int64_t)max(page[q >> 1], 0) * a.c.kv_heads + head) * a.c.page_size + (t & (a.c.page_size - 1))) * D;
-#pragma unroll
-                for (int b = 0; b < S::kSlabs; ++b) x[q * S::kSlabs + b] = __ldg(reinterpret_cast<const uint4 *>(from) + b * 4 + pc);
-            }
-        };
-        auto store = [&](uint32_t to, const uint4 (&x)[kPieces]) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int t = 32 * w + 8 * q + r;
-#pragma unroll
-                for (int b = 0; b < S::kSlabs; ++b) {
-                    const uint4 c = x[q * S::kSlabs + b];
-                    uint4 lo, hi;
-                    codes_to_half(c.x ^ 0x80808080u, lo.x, lo.y);
-                    codes_to_half(c.y ^ 0x80808080u, lo.z, lo.w);
-                    codes_to_half(c.z ^ 0x80808080u, hi.x, hi.y);
-                    codes_to_half(c.w ^ 0x80808080u, hi.z, hi.w);
-                    const uint32_t line = to + b * S::kSlab + t * 128;
-                    ptx::st_shared_v4(line + (((2 * pc) ^ (t & 7)) << 4), lo);
-                    ptx::st_shared_v4(line + (((2 * pc + 1) ^ (t & 7)) << 4), hi);
-                }
-            }
-        };
-        // scales of the 16 tokens that thread ct < 8 looks after
-        auto scales = [&](int j) {
-            const int page = attend_page(a, i, min(j * kTlBlock + 16 * ct, max(len - 1, 0)));
-            const int64_t block = (int64_t)max(page, 0) * a.c.kv_heads + head;
-            const float nan = __uint_as_float(0x7fc00000u);
-            return make_float2(page < 0 ? nan : __ldg(a.c.k_scale + block), page < 0 ? nan : __ldg(a.c.v_scale + block));
-        };
-        uint4 xk[kPieces], xv[kPieces];
-        int page[2];
-        float2 sc = make_float2(0.f, 0.f);
-        if (most > 0) {
-            page[0] = page_of(0, 0);
-            page[1] = page_of(0, 1);
-            load(a.c.k, 0, page, xk);
-            load(a.c.v, 0, page, xv);
-            if (ct < kTlGroups) sc = scales(0);
-        }
+        // a thread's pieces: 16 codes of token 32 w + 8 q + lane / 4, piece lane % 4 of each slab, odd tokens the slabs in the other
+        // order: eight neighbouring lanes read and write eight different places of 128 bytes
+        const int w = warp - 8, r = lane >> 2, pc = lane & 3;
+        TlItem t;
         bool ok = true;
-        for (int j = 0; j < most; ++j) {
-            const int s = j & 1, more = j + 1 < most;
-            if (more) {
-                page[0] = page_of(j + 1, 0);
-                page[1] = page_of(j + 1, 1);
+        uint32_t n = 0, copy = 0;
+#pragma unroll 1
+        for (uint32_t item = 0; ok && (ok = tl_take(sh, item, t)) && t.i >= 0; ++item) {
+            const int most = max(t.blocks[0], t.blocks[1]);
+#pragma unroll 1
+            for (int j = 0; ok && j < 2 * most; ++j, ++copy) {
+                const bool values = j & 1;           // keys of a block, then its values
+                const uint32_t slot = copy % S::kSlots, s = n & 1;
+                ok = ptx::mbar_wait(&sh->code_full[slot], copy / S::kSlots & 1);
+                if (!ok) break;
+                uint4 x[4 * S::kSlabs];
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int b = 0; b < S::kSlabs; ++b)
+                        x[q * S::kSlabs + b] = ld_shared_u4(code_u32 + slot * S::kSlot + (32 * w + 8 * q + r) * D + ((b ^ (S::kSlabs > 1 ? r & 1 : 0)) * 4 + pc) * 16);
+                ptx::mbar_arrive(&sh->code_empty[slot]);
+                if (n >= 2) ok = ptx::mbar_wait(values ? &sh->v_empty[s] : &sh->k_empty[s], ((n >> 1) - 1) & 1);
+                if (!ok) break;
+                const uint32_t to = (values ? v_u32 : k_u32) + s * S::kOperand;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int tk = 32 * w + 8 * q + r;
+#pragma unroll
+                    for (int b = 0; b < S::kSlabs; ++b) {
+                        const uint4 c = x[q * S::kSlabs + b];
+                        uint4 lo, hi;
+                        codes_to_half(c.x ^ 0x80808080u, lo.x, lo.y);
+                        codes_to_half(c.y ^ 0x80808080u, lo.z, lo.w);
+                        codes_to_half(c.z ^ 0x80808080u, hi.x, hi.y);
+                        codes_to_half(c.w ^ 0x80808080u, hi.z, hi.w);
+                        const uint32_t line = to + (b ^ (S::kSlabs > 1 ? r & 1 : 0)) * S::kSlab + tk * 128;
+                        ptx::st_shared_v4(line + (((2 * pc) ^ (tk & 7)) << 4), lo);
+                        ptx::st_shared_v4(line + (((2 * pc + 1) ^ (tk & 7)) << 4), hi);
+                    }
+                }
+                ptx::fence_proxy_async_smem();
+                ptx::mbar_arrive(values ? &sh->v_full[s] : &sh->k_full[s]);
+                n += values;
             }
-            if (j >= 2 && !(ok = ptx::mbar_wait(&sh->k_empty[s], ((j >> 1) - 1) & 1))) break;
-            store(k_u32 + s * S::kOperand, xk);
-            if (ct < kTlGroups) {
-                float lv, inv;
-                value_scale(sc.y, lv, inv);
-                sh->group[j & 3][ct] = make_float4(sc.x, lv, inv, 0.f);
-            }
-            ptx::fence_proxy_async_smem();
-            ptx::mbar_arrive(&sh->k_full[s]);
-            if (more) {
-                load(a.c.k, j + 1, page, xk);
-                if (ct < kTlGroups) sc = scales(j + 1);
-            }
-            if (j >= 2 && !(ok = ptx::mbar_wait(&sh->v_empty[s], ((j >> 1) - 1) & 1))) break;
-            store(v_u32 + s * S::kOperand, xv);
-            ptx::fence_proxy_async_smem();
-            ptx::mbar_arrive(&sh->v_full[s]);
-            if (more) load(a.c.v, j + 1, page, xv);
         }
         if (!ok) sh->gave_up = 1;
     } else {
         // ---------------- a row per thread -------------------------------------------------------------------
-        regs_more<kTlSoftRegs>();
-        const int x = warp >> 2, r = tid & 127, m = m0 + x * kTlRows + r, j_row = m / a.group;
-        const bool real = m < rows;
-        const uint32_t q_row = s_u32 + x * S::kOperand + r * 128;
-        const int64_t o_row = (int64_t)(row0 + j_row) * a.q_heads + head * a.group + (m - j_row * a.group);
-        float factor = 0.f;
-        {
-            uint4 raw[D / 8];
-            float top = 0.f;
-            const uint4 *p = reinterpret_cast<const uint4 *>(a.q + (int64_t)(row0 + j_row) * a.q_stride +
-                                                             (int64_t)(head * a.group + (m - j_row * a.group)) * D);
-#pragma unroll
-            for (int e = 0; e < D / 8; ++e) raw[e] = real ? __ldg(p + e) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-            for (int e = 0; e < D / 8; ++e) {
-                float f[8];
-                Elem<__nv_bfloat16>::unpack(raw[e], f);
-#pragma unroll
-                for (int z = 0; z < 8; ++z) top = max_nan(top, fabsf(f[z]));
-            }
-            float unit = query_scale(top, a.scale_log2, factor);
-            if (factor < 0.f) {                      // the scores' factor is positive: the largest sum is the largest score
-                factor = -factor;
-                unit = -unit;
-            }
-#pragma unroll
-            for (int e = 0; e < D / 8; ++e) {
-                float f[8];
-                Elem<__nv_bfloat16>::unpack(raw[e], f);
-                uint4 h = make_uint4(pack_half(f[0] * unit, f[1] * unit), pack_half(f[2] * unit, f[3] * unit),
-                                     pack_half(f[4] * unit, f[5] * unit), pack_half(f[6] * unit, f[7] * unit));
-                ptx::st_shared_v4(q_row + (e >> 3) * S::kSlab + (((e & 7) ^ (r & 7)) << 4), h);
-            }
-            ptx::fence_proxy_async_smem();
-            ptx::mbar_arrive(&sh->q_full);
-        }
-        const int end = a.causal ? min(len, len - n + 1 + min(m, rows - 1) / a.group) : len;
-        // the first row of the warp sees the fewest tokens
-        const int warp_end = a.causal ? min(len, len - n + 1 + min(m - lane, rows - 1) / a.group) : len;
-        const uint32_t lanes = (uint32_t)(warp & 3) << 21, t_s = tmem + lanes + x * 128, t_o = tmem + lanes + 256 + x * D;
-        float top = kAtNothing, l = 0.f;
+        const int x = warp >> 2, r = tid & 127, jj = r / a.group, r_head = r - jj * a.group;   // a row's token of the tile, and its head
+        const uint32_t q_tile = s_u32 + x * S::kOperand, lanes = (uint32_t)(warp & 3) << 21;
+        const uint32_t t_s = tmem + lanes + x * 128, t_o = tmem + lanes + 256 + x * D;
+        constexpr int kLanes = D / 8;                // lanes of a row when a warp takes whole rows, 16 bytes a lane
+        constexpr int kRowsAt = 32 / kLanes;
         bool ok = true;
-        for (int j = 0; j < blocks[x]; ++j) {
-            if (!(ok = ptx::mbar_wait(&sh->s_full[x], j & 1))) break;
-            ptx::tc_fence_after();
-            const float4 *group = sh->group[j & 3];
-            const int left = end - j * kTlBlock;     // tokens of the block that the row sees
-            const bool masked = (j + 1) * kTlBlock > warp_end;
-            // ---- the row's maximum (of s', with the values' scale)
-            uint32_t v[kTlBlock];
-#pragma unroll
-            for (int c = 0; c < kTlBlock / 32; ++c) ptx::tmem_ld32(t_s + c * 32, *reinterpret_cast<uint32_t (*)[32]>(v + c * 32));
-            ptx::tmem_ld_wait();
-            float now = kAtNothing;
-#pragma unroll
-            for (int c = 0; c < kTlGroups; ++c) {
-                float most_s = -INFINITY;
+        uint32_t n = 0, turns = 0, items = 0, items_q = 0;     // blocks; this tile's blocks, items and queries so far
+        // the item in work: what of it outlives the look at the next one
+        int mine = -1, end = 0, blocks = 0, most = 0;
+        float factor = 0.f;                          // of the row's scores
+        bool has = false, bad = false;
+#pragma unroll 1
+        for (uint32_t item = 0;; ++item) {
+            float top = kAtNothing, l = 0.f;
+            const int warp_end = __shfl_sync(0xffffffffu, end, 0);      // the first row of the warp sees the fewest tokens
+#pragma unroll 1
+            for (int j = 0; ok && j < blocks; ++j, ++turns) {
+                if (!(ok = ptx::mbar_poll(&sh->s_full[x], turns & 1))) break;
+                ptx::tc_fence_after();
+                const float4 *group = sh->group[(n + j) % kTlGroupRing];
+                const int left = end - j * kTlBlock; // tokens of the block that the row sees
+                const bool masked = (j + 1) * kTlBlock > warp_end;
+                float now = kAtNothing;              // the row's maximum (of s', with the values' scale)
+                uint32_t va[32], vb[32];
                 if (masked) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) most_s = fmaxf(most_s, 16 * c + e < left ? __uint_as_float(v[16 * c + e]) : -INFINITY);
+                    now = careful_top(group, factor, left, t_s);
                 } else {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) most_s = fmaxf(most_s, __uint_as_float(v[16 * c + e]));
+                    ptx::tmem_ld32(t_s, va);
+                    ptx::tmem_ld_wait();
+                    ptx::tmem_ld32(t_s + 32, vb);
+                    now = tile_top(va, group, factor, now);
+                    ptx::tmem_ld_wait();
+                    ptx::tmem_ld32(t_s + 64, va);
+                    now = tile_top(vb, group + 2, factor, now);
+                    ptx::tmem_ld_wait();
+                    ptx::tmem_ld32(t_s + 96, vb);
+                    now = tile_top(va, group + 4, factor, now);
+                    ptx::tmem_ld_wait();
+                    now = tile_top(vb, group + 6, factor, now);
                 }
-                const float4 g = group[c];
-                now = fmaxf(now, fmaf(most_s, factor * g.x, g.y));
-            }
-            if (__any_sync(0xffffffffu, now - top > kAtSlack)) {
-                const float next = fmaxf(top, now), k = ex2(top - next);
-                top = next;
-                l *= k;
-                if (j > 0) {
+                if (__any_sync(0xffffffffu, now - top > kAtSlack)) {
+                    const float to = fmaxf(top, now), k = ex2(top - to);
+                    top = to;
+                    l *= k;
+                    if (j > 0) {
+#pragma unroll 1
+                        for (int c = 0; c < D / 16; ++c) {
+                            uint32_t o[16];
+                            ptx::tmem_ld16(t_o + c * 16, o);
+                            ptx::tmem_ld_wait();
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) {
-                        uint32_t v[16];
-                        ptx::tmem_ld16(t_o + c * 16, v);
-                        ptx::tmem_ld_wait();
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * k);
-                        tmem_st16(t_o + c * 16, v);
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * k);
+                            tmem_st16(t_o + c * 16, o);
+                        }
                     }
                 }
+                if (masked || __any_sync(0xffffffffu, fabsf(top) > kTlLarge)) {
+                    careful_weights(group, factor, top, left, t_s, l);
+                } else {
+                    ptx::tmem_ld32(t_s, va);
+                    ptx::tmem_ld_wait();
+                    ptx::tmem_ld32(t_s + 32, vb);
+                    tile_weights(va, group, factor, top, t_s, l);
+                    ptx::tmem_ld_wait();
+                    ptx::tmem_ld32(t_s + 64, va);
+                    tile_weights(vb, group + 2, factor, top, t_s + 16, l);
+                    ptx::tmem_ld_wait();
+                    ptx::tmem_ld32(t_s + 96, vb);
+                    tile_weights(va, group + 4, factor, top, t_s + 32, l);
+                    ptx::tmem_ld_wait();
+                    tile_weights(vb, group + 6, factor, top, t_s + 48, l);
+                }
+                tmem_st_wait();
+                ptx::tc_fence_before();
+                ptx::mbar_arrive(&sh->p_full[x]);
             }
-            // ---- weights
-            if (masked || __any_sync(0xffffffffu, fabsf(top) > kTlLarge)) tile_weights<true>(v, group, factor, top, left, t_s, l);
-            else tile_weights<false>(v, group, factor, top, left, t_s, l);
-            tmem_st_wait();
-            ptx::tc_fence_before();
-            ptx::mbar_arrive(&sh->p_full[x]);
-        }
-        if (!ok) sh->gave_up = 1;
-        // ---- out
-        if (most > 0 && !ptx::mbar_wait(&sh->o_full, 0)) sh->gave_up = 1;
-        ptx::tc_fence_after();
-        const bool nan = len < 0 || sh->gave_up;
-        const float k = nan ? __uint_as_float(0x7fc00000u) : l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-            uint32_t v[16];
-            ptx::tmem_ld16(t_o + c * 16, v);
-            ptx::tmem_ld_wait();
-            uint4 o[2];
-            __nv_bfloat162 *h = reinterpret_cast<__nv_bfloat162 *>(o);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)              // (a tile that saw no block has no sums: what TMEM holds is not used)
-                h[e] = blocks[x] > 0 || nan ? __floats2bfloat162_rn(__uint_as_float(v[2 * e]) * k, __uint_as_float(v[2 * e + 1]) * k)
-                                            : __floats2bfloat162_rn(0.f, 0.f);
-            // over the queries (all MMAs are done), swizzled alike
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int ch = 2 * c + e;
-                ptx::st_shared_v4(q_row + (ch >> 3) * S::kSlab + (((ch & 7) ^ (r & 7)) << 4), o[e]);
+            n += most;
+            // ---- the next item's queries, while this one's last products run: scaled, to fp16 in the operand's layout, in place.  (The
+            // tile's queries before are done with: the last scores of theirs have come.)
+            TlItem next;
+            if (!tl_take(sh, item, next)) {
+                ok = false;
+                sh->gave_up = 1;
+                next.i = -1;
             }
-        }
-        if (real && a.lse) a.lse[o_row] = nan ? k : l == 0.f ? -INFINITY : (top + log2f(l)) * kAtLn2;
-        __syncwarp();
-        // whole rows, 16 bytes a lane
-        constexpr int kLanes = D / 8;                // lanes of a row
-        const int first = m0 + x * kTlRows + (r & ~31);
-#pragma unroll 4
-        for (int y = lane / kLanes; y < 32; y += 32 / kLanes) {
-            const int mm = first + y, ch = lane % kLanes, rr = (r & ~31) + y;
-            if (mm < rows) {
-                const int jj = mm / a.group;
-                const int64_t row = (int64_t)(row0 + jj) * a.q_heads + head * a.group + (mm - jj * a.group);
-                const float4 o = ptx::ld_shared_v4(s_u32 + x * S::kOperand + rr * 128 + (ch >> 3) * S::kSlab + (((ch & 7) ^ (rr & 7)) << 4));
-                *reinterpret_cast<float4 *>(a.out + row * D + ch * 8) = o;
+            int mine_next = -1, end_next = 0;
+            float factor_next = 0.f;
+            if (next.i >= 0) {
+                const int j_row = next.j0 + x * tile_tokens + jj;
+                if (jj < tile_tokens && j_row < next.n) mine_next = (next.row0 + j_row) * a.q_heads + next.head * a.group + r_head;
+                end_next = a.causal ? next.len - next.n + 1 + min(j_row, next.n - 1) : next.len;
             }
+            const int blocks_next = next.i < 0 ? 0 : x ? next.blocks[1] : next.blocks[0];
+            if (ok && blocks_next > 0) {
+                if (!(ok = ptx::mbar_wait(&sh->q_raw[x], items_q & 1))) sh->gave_up = 1;
+                ++items_q;
+                // a warp's step: 16 lanes (D = 64: 8) a row
+#pragma unroll 1
+                for (int e = 0; e < 32; e += 4 * kRowsAt) {
+                    uint4 raw[4];
+                    const int ch = lane % kLanes;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int rr = e + g * kRowsAt + lane / kLanes;
+                        const bool real = __shfl_sync(0xffffffffu, mine_next, rr) >= 0;
+                        raw[g] = ld_shared_u4(q_tile + (ch >> 3) * S::kSlab + ((r & ~31) + rr) * 128 + (((ch & 7) ^ (rr & 7)) << 4));
+                        if (!real) raw[g] = make_uint4(0u, 0u, 0u, 0u);
+                    }
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        // the row's largest |q|, on the bf16 bits: of 8 elements, then over the row's lanes
+                        uint32_t w = max2_nan(max2_nan(raw[g].x & 0x7fff7fffu, raw[g].y & 0x7fff7fffu), max2_nan(raw[g].z & 0x7fff7fffu, raw[g].w & 0x7fff7fffu));
+                        w = max2_nan(w, w >> 16);
+#pragma unroll
+                        for (int o = kLanes / 2; o > 0; o >>= 1) w = max2_nan(w, __shfl_xor_sync(0xffffffffu, w, o));
+                        float f[8], factor_q;
+                        float unit = query_scale(__uint_as_float(w << 16), a.scale_log2, factor_q);
+                        if (factor_q < 0.f) {        // the scores' factor is positive: the largest sum is the largest score
+                            factor_q = -factor_q;
+                            unit = -unit;
+                        }
+                        Elem<__nv_bfloat16>::unpack(raw[g], f);
+                        const int rr = (r & ~31) + e + g * kRowsAt + lane / kLanes;
+                        factor_q = __shfl_sync(0xffffffffu, factor_q, lane % kRowsAt * kLanes);    // to the row's own thread
+                        if (lane / kRowsAt == e / kRowsAt + g) factor_next = factor_q;
+                        ptx::st_shared_v4(q_tile + (ch >> 3) * S::kSlab + rr * 128 + (((ch & 7) ^ (rr & 7)) << 4),
+                                          make_uint4(pack_half(f[0] * unit, f[1] * unit), pack_half(f[2] * unit, f[3] * unit),
+                                                     pack_half(f[4] * unit, f[5] * unit), pack_half(f[6] * unit, f[7] * unit)));
+                    }
+                }
+                ptx::fence_proxy_async_smem();
+                ptx::mbar_arrive(&sh->q_full[x]);
+            }
+            // ---- out
+            if (has) {
+                const bool any = blocks > 0;
+                if (any && ok) {
+                    ok = ptx::mbar_wait(&sh->o_full[x], items & 1);
+                    ++items;
+                }
+                if (!ok) sh->gave_up = 1;
+                ptx::tc_fence_after();
+                const bool nan = bad || sh->gave_up;
+                const float k = nan ? __uint_as_float(0x7fc00000u) : l == 0.f ? 0.f : 1.f / l;
+                __nv_bfloat16 *to = a.out + (int64_t)max(mine, 0) * D;
+#pragma unroll 1
+                for (int b = 0; b < D / 32; ++b) {
+                    uint32_t v[32];
+                    ptx::tmem_ld32(t_o + b * 32, v);
+                    ptx::tmem_ld_wait();
+                    if (b == D / 32 - 1 && any) {
+                        ptx::tc_fence_before();
+                        ptx::mbar_arrive(&sh->o_empty[x]);
+                    }
+                    uint32_t o[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(v[2 * e]) * k, __uint_as_float(v[2 * e + 1]) * k);
+                        o[e] = any || nan ? *reinterpret_cast<const uint32_t *>(&h) : 0u;      // a tile that saw no block has no sums
+                    }
+                    if (mine >= 0) {
+                        st_global_v8(to + b * 32, o);
+                        st_global_v8(to + b * 32 + 16, o + 8);
+                    }
+                }
+                if (mine >= 0 && a.lse) a.lse[mine] = nan ? k : l == 0.f ? -INFINITY : (top + log2f(l)) * kAtLn2;
+            }
+            if (next.i < 0) break;
+            has = true;
+            bad = next.len < 0;
+            mine = mine_next;
+            end = end_next;
+            factor = factor_next;
+            blocks = blocks_next;
+            most = max(next.blocks[0], next.blocks[1]);
         }
         ptx::tc_fence_before();
     }
