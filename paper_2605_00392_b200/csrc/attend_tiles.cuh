@@ -8,9 +8,10 @@
 // One CTA per SM takes items (two tiles) blockIdx.x, + gridDim.x, ...; what its warps do:
 //   0-3, 4-7  a row per thread of the first and second tile: softmax, output; and the next item's queries from bf16 to fp16, in place
 //   8-11      codes to fp16 in the swizzled operand layout (tiles of (token, 64 elements), K-major for the keys, MN-major for the values)
-//   12        issues the MMAs    13  finds the items    14  bulk copies of codes    15  the queries, by TMA
-// While one tile's softmax runs, the other's MMAs do; S of a tile's next block is issued behind the PV of this one, whose P it
-// overwrites.  One item's output leaves while the next one's scores are computed.
+//   12, 13    issue the MMAs of the first and second tile, in turns (one warp for both was the pace of the kernel)    14  bulk copies of codes    15  finds the items and fetches their queries, by TMA
+// S of a tile's next block is issued behind the PV of this one, whose P it overwrites.  The tiles take turns: one's PV and S, then the
+// other's, so that one's softmax runs beside the other's MMAs (left to themselves they fell into step, both softmaxes, then
+// both MMAs: 4850 cycles a block).  One item's output leaves while the next one's scores are computed.
 // Everything large comes by bulk copies: with 227 KB of shared memory there are some 20 KB of L1 left, and ordinary loads of
 // 64 KB of queries, which need a line of it each while they are on their way, took 10,000 cycles.
 // A row's sums are rescaled only when its maximum has grown by more than 2^8 (the weights have that room in fp16).
@@ -26,7 +27,7 @@ constexpr int kTlTiles = 2;
 constexpr int kTlBlock = 128;                        // tokens of a block
 constexpr int kTlSoft = kTlTiles * kTlRows;
 constexpr int kTlThreads = kTlSoft + 128 + 128;     // (the last warp only makes it 128 registers a thread)
-constexpr int kTlSoftRegs = 168, kTlCodeRegs = 88, kTlOtherRegs = 88;    // registers of a thread: 2, 1, 1 of four warpgroups
+constexpr int kTlSoftRegs = 184, kTlCodeRegs = 72, kTlOtherRegs = 72;    // registers of a thread: 2, 1, 1 of four warpgroups
 static_assert(2 * kTlSoftRegs + kTlCodeRegs + kTlOtherRegs <= 4 * 128, "what the block was launched with");
 constexpr int kTlGroups = kTlBlock / 16;             // a page holds at least 16 tokens: scales are per 16
 
@@ -57,7 +58,7 @@ struct TlShared {
     uint64_t code_full[4], code_empty[4];            // keys of block 0, values of block 0, keys of block 1, ...
     uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
     uint64_t q_raw[kTlTiles], q_full[kTlTiles], q_empty[kTlTiles], s_full[kTlTiles], p_full[kTlTiles], o_full[kTlTiles], o_empty[kTlTiles];
-    uint64_t done;
+    uint64_t turn[kTlTiles], done;
     uint32_t tmem;
     volatile int gave_up;
 };
@@ -152,9 +153,9 @@ __device__ inline float max16(const float (&s)[16])
     return max3(max3(a, b, c), max3(d, s[12], s[13]), fmaxf(s[14], s[15]));
 }
 
-// The largest s' of 32 of a row's scores (two groups), and their weights to the place `to` in TMEM, the sum of these (without the values'
-// scale) into l.  The scores come from TMEM once for each, 32 at a time: a thread that keeps its 128 spills whatever else it has,
-// and what is spilled comes back from L2 (shared memory has left L1 next to nothing).
+// The largest s' of 32 of a row's scores (two groups), and their weights p, the sum of these (without the values' scale) into l, the largest
+// s' - top into `most`.  The scores come from TMEM 32 at a time: a thread that keeps its 128 spills whatever else it has, and what is
+// spilled comes back from L2 (shared memory has left L1 next to nothing).
 __device__ inline float tile_top(const uint32_t (&v)[32], const float4 *group, float factor, float now)
 {
 #pragma unroll
@@ -167,29 +168,30 @@ __device__ inline float tile_top(const uint32_t (&v)[32], const float4 *group, f
     }
     return now;
 }
-__device__ inline void tile_weights(const uint32_t (&v)[32], const float4 *group, float factor, float top, uint32_t to, float &l)
+__device__ inline void tile_weights(const uint32_t (&v)[32], const float4 *group, float factor, float top, uint32_t *p, float &most, float &l)
 {
-    uint32_t p[16];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const float4 g = group[h];
         const float k = factor * g.x, b = g.y - top;
         const uint64_t k2 = pack2(k, k), b2 = pack2(b, b);
         uint64_t sum2 = 0;
+        float w[16];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2)
+            unpack2(fma2(pack2(__uint_as_float(v[16 * h + e]), __uint_as_float(v[16 * h + e + 1])), k2, b2), w[e], w[e + 1]);
+        most = fmaxf(most, max16(w));
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
-            float w0, w1;
-            unpack2(fma2(pack2(__uint_as_float(v[16 * h + e]), __uint_as_float(v[16 * h + e + 1])), k2, b2), w0, w1);
-            w0 = ex2(w0);
-            w1 = ex2(w1);
-            sum2 = add2(sum2, pack2(w0, w1));
-            p[8 * h + e / 2] = pack_half(w0, w1);
+            w[e] = ex2(w[e]);
+            w[e + 1] = ex2(w[e + 1]);
+            sum2 = add2(sum2, pack2(w[e], w[e + 1]));
+            p[8 * h + e / 2] = pack_half(w[e], w[e + 1]);
         }
         float s0, s1;
         unpack2(sum2, s0, s1);
         l = fmaf(s0 + s1, g.z, l);
     }
-    tmem_st16(to, p);
 }
 // The same where tokens from `left` on are not seen, or scores are so large that their own rounding matters: it is what the maximum
 // went through, so they go through it too before the maximum is taken off.  Loops of few instructions, from TMEM again.
@@ -258,9 +260,9 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         }
         for (int s = 0; s < 2; ++s) {
             ptx::mbar_init(&sh->k_full[s], 128);
-            ptx::mbar_init(&sh->k_empty[s], 1);
+            ptx::mbar_init(&sh->k_empty[s], kTlTiles);
             ptx::mbar_init(&sh->v_full[s], 128);
-            ptx::mbar_init(&sh->v_empty[s], 1);
+            ptx::mbar_init(&sh->v_empty[s], kTlTiles);
         }
         for (int x = 0; x < kTlTiles; ++x) {
             ptx::mbar_init(&sh->q_raw[x], 1);
@@ -270,8 +272,9 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             ptx::mbar_init(&sh->p_full[x], kTlRows);
             ptx::mbar_init(&sh->o_full[x], 1);
             ptx::mbar_init(&sh->o_empty[x], kTlRows);
+            ptx::mbar_init(&sh->turn[x], 1);
         }
-        ptx::mbar_init(&sh->done, 1);
+        ptx::mbar_init(&sh->done, kTlTiles);
         sh->gave_up = 0;
         ptx::fence_mbar_init();
     }
@@ -289,17 +292,18 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     // (not earlier: a kernel behind this one that takes TMEM before it waits could otherwise have it first)
     ptx::grid_dep_launch();
 
-    // (each warpgroup by one instruction of its own)
-    if (warp >= 12) regs_fewer<kTlOtherRegs>();
-    else if (warp >= 8) regs_fewer<kTlCodeRegs>();
-    else regs_more<kTlSoftRegs>();
-    if (warp == 13) {
-        // ---------------- the work: items blockIdx.x, + gridDim.x, ... that have rows ------------------------
+    // (registers: one instruction for each warpgroup, ahead of all that the warpgroup does)
+    if (warp >= 12) {
+    regs_fewer<kTlOtherRegs>();
+    if (warp == 15) {
+        // ---------------- the work: items blockIdx.x, + gridDim.x, ... that have rows; their queries, as they are, in the operand's
+        // layout already
         const int per = a.batch * a.c.kv_heads, all = row_blocks * per;
-        uint32_t k = 0;
         int at = blockIdx.x;
+        bool ok = true;
+        uint32_t uses[kTlTiles] = {0, 0};
 #pragma unroll 1
-        for (bool ok = true; ok; ++k) {
+        for (uint32_t k = 0; ok; ++k) {
             TlItem t;
             t.i = -1;
             // 32 of the numbers at a time, one per lane (bounds that are far above the requests' lengths leave most of them empty)
@@ -319,36 +323,47 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                 if (found) {
                     const int from = __ffs(found) - 1;
                     at += (from + 1) * gridDim.x;
-                    if (lane == from) {
-#pragma unroll 1
-                        for (int x = 0; x < kTlTiles; ++x) {
-                            const int first = t.j0 + x * tile_tokens, last = min(first + tile_tokens, t.n) - 1;
-                            const int end = first >= t.n || t.len < 0 ? 0 : a.causal ? t.len - t.n + 1 + last : t.len;
-                            const int b = (max(end, 0) + kTlBlock - 1) / kTlBlock;
-                            if (x) t.blocks[1] = b;
-                            else t.blocks[0] = b;
-                        }
-                    }
                     t.i = __shfl_sync(0xffffffffu, t.i, from);
                     t.head = __shfl_sync(0xffffffffu, t.head, from);
                     t.j0 = __shfl_sync(0xffffffffu, t.j0, from);
                     t.row0 = __shfl_sync(0xffffffffu, t.row0, from);
                     t.n = __shfl_sync(0xffffffffu, t.n, from);
                     t.len = __shfl_sync(0xffffffffu, t.len, from);
-                    t.blocks[0] = __shfl_sync(0xffffffffu, t.blocks[0], from);
-                    t.blocks[1] = __shfl_sync(0xffffffffu, t.blocks[1], from);
+#pragma unroll
+                    for (int x = 0; x < kTlTiles; ++x) {
+                        const int first = t.j0 + x * tile_tokens, last = min(first + tile_tokens, t.n) - 1;
+                        const int end = first >= t.n || t.len < 0 ? 0 : a.causal ? t.len - t.n + 1 + last : t.len;
+                        t.blocks[x] = (max(end, 0) + kTlBlock - 1) / kTlBlock;
+                    }
                     break;
                 }
                 t.i = -1;
             }
-            if (k >= kTlItems) ok = ptx::mbar_wait(&sh->item_empty[k % kTlItems], (k / kTlItems - 1) & 1);
+            if (k >= kTlItems) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&sh->item_empty[k % kTlItems], (k / kTlItems - 1) & 1));
             if (ok && lane == 0) {
                 sh->item[k % kTlItems] = t;
                 ptx::mbar_arrive(&sh->item_full[k % kTlItems]);
             }
-            if (!ok) sh->gave_up = 1;
             if (t.i < 0) break;
+#pragma unroll
+            for (int x = 0; x < kTlTiles; ++x) {
+                if (!ok || t.blocks[x] == 0) continue;
+                if (uses[x] > 0) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&sh->q_empty[x], (uses[x] - 1) & 1));
+                if (ok && lane == 0) {
+                    ptx::mbar_arrive_expect_tx(&sh->q_raw[x], (uint32_t)(S::kSlabs * tile_tokens * a.group * 128));
+                    for (int b = 0; b < S::kSlabs; ++b)
+                        ptx::tma_load_3d(s_u32 + x * S::kOperand + b * S::kSlab, &map_q, &sh->q_raw[x], b * 64, t.head * a.group,
+                                         t.row0 + t.j0 + x * tile_tokens);
+                }
+                __syncwarp();
+                if (ok) ++uses[x];
+            }
         }
+        if (!ok) sh->gave_up = 1;
+        // no copy is left on its way into memory that this CTA gives back
+#pragma unroll
+        for (int x = 0; x < kTlTiles; ++x)
+            if (uses[x] > 0) ptx::mbar_wait(&sh->q_raw[x], (uses[x] - 1) & 1);
     } else if (warp == 14) {
         // ---------------- codes of the items' blocks, and their scales ----------------------------------------
         const int per_page = min(a.c.page_size, kTlBlock), copies = kTlBlock / per_page;   // a page of a head is one piece of memory
@@ -391,114 +406,79 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         // no copy is left on its way into memory that this CTA gives back
         for (uint32_t c = copy > S::kSlots ? copy - S::kSlots : 0; c < copy; ++c)
             ptx::mbar_wait(&sh->code_full[c % S::kSlots], c / S::kSlots & 1);
-    } else if (warp == 15) {
-        // ---------------- the coming items' queries, as they are, in the operand's layout already ---------------
-        TlItem t;
+    } else {
+        // ---------------- the MMAs of tile x ----------------------------------------------------------------
+        // the whole warp walks the blocks, one elected lane issues
+        const int x = warp - 12;
+        const bool issuer = elect_one();
+        const uint32_t id_s = idesc_f16(kTlRows, kTlBlock, false), id_o = idesc_f16(kTlRows, D, true);
+        const uint32_t t_s = tmem + x * 128, t_o = tmem + 256 + x * D;
+        // descriptors differ from these by multiples of 16 bytes in the address (their low 14 bits, which never carry)
+        const uint64_t d_q = ptx::smem_desc_sw128(s_u32 + x * S::kOperand, 16, 1024), d_k = ptx::smem_desc_sw128(k_u32, 16, 1024);
+        const uint64_t d_v = ptx::smem_desc_sw128(v_u32, S::kSlab, 1024);
         bool ok = true;
-        uint32_t uses[kTlTiles] = {0, 0};
+        uint32_t n = 0, step = 0, items = 0, turns = 0;      // blocks and steps; this tile's items and blocks so far
+        TlItem t;
 #pragma unroll 1
         for (uint32_t item = 0; ok && (ok = tl_take(sh, item, t)) && t.i >= 0; ++item) {
+            const int most = max(t.blocks[0], t.blocks[1]), mine = x ? t.blocks[1] : t.blocks[0];
+            // step j: products of block j - 1, scores of block j; n is block j's number.  A block that this tile sees nothing of is passed on
+            // once it is there (not before: its buffer's turns would be mixed up)
 #pragma unroll 1
-            for (int x = 0; ok && x < kTlTiles; ++x) {
-                if ((x ? t.blocks[1] : t.blocks[0]) == 0) continue;
-                const uint32_t before = x ? uses[1] : uses[0];
-                if (before > 0) ok = ptx::mbar_wait(&sh->q_empty[x], (before - 1) & 1);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                if (lane == 0) {
-                    ptx::mbar_arrive_expect_tx(&sh->q_raw[x], (uint32_t)(S::kSlabs * tile_tokens * a.group * 128));
-                    for (int b = 0; b < S::kSlabs; ++b)
-                        ptx::tma_load_3d(s_u32 + x * S::kOperand + b * S::kSlab, &map_q, &sh->q_raw[x], b * 64, t.head * a.group,
-                                         t.row0 + t.j0 + x * tile_tokens);
+            for (int j = 0; j <= most && most > 0; ++j, ++n, ++step) {
+                const uint32_t s = n & 1, s_before = s ^ 1;
+                const bool products = j > 0 && j <= mine, scores = j < mine;
+                // what is there early is waited for first, the weights last: their way to the next scores is the kernel's longest
+                if (j > 0) ok = ptx::mbar_wait(&sh->v_full[s_before], ((n - 1) >> 1) & 1);
+                if (j < most) ok = ok && ptx::mbar_wait(&sh->k_full[s], (n >> 1) & 1);
+                if (j == 0 && mine > 0) ok = ok && ptx::mbar_wait(&sh->q_full[x], items & 1);
+                if (j == 1 && mine > 0 && items > 0) ok = ok && ptx::mbar_wait(&sh->o_empty[x], (items - 1) & 1);   // (the last item's output is out of TMEM)
+                // the other tile's turn before this
+                if (x > 0 || step > 0) ok = ok && ptx::mbar_wait(&sh->turn[x ^ 1], (x ? step : step - 1) & 1);
+                if (products) {
+                    ok = ok && ptx::mbar_wait(&sh->p_full[x], turns & 1);
+                    ++turns;
                 }
+                if (!ok) break;
+                ptx::tc_fence_after();
+                if (products && issuer) {
+                    const uint64_t v0 = d_v + s_before * (S::kOperand >> 4);
+#pragma unroll
+                    for (int k = 0; k < kTlBlock / 16; ++k) umma_f16_ts(t_o, t_s + k * 8, v0 + k * (2048 >> 4), id_o, j - 1 + k > 0);
+                    ptx::umma_commit(&sh->v_empty[s_before]);
+                    if (j == mine) ptx::umma_commit(&sh->o_full[x]);
+                } else if (j > 0 && issuer) {
+                    ptx::mbar_arrive(&sh->v_empty[s_before]);
+                }
+                if (j < most) {
+                    if (scores && issuer) {
+                        const uint64_t k0 = d_k + s * (S::kOperand >> 4);
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k) {
+                            const int at = ((k >> 2) * S::kSlab + (k & 3) * 32) >> 4;
+                            ptx::umma_bf16(t_s, d_q + at, k0 + at, id_s, k > 0);
+                        }
+                        ptx::umma_commit(&sh->s_full[x]);
+                        ptx::umma_commit(&sh->k_empty[s]);
+                        if (j + 1 == mine) ptx::umma_commit(&sh->q_empty[x]);
+                    } else if (issuer) {
+                        ptx::mbar_arrive(&sh->k_empty[s]);
+                    }
+                }
+                if (issuer) ptx::mbar_arrive(&sh->turn[x]);
                 __syncwarp();
-                if (x) ++uses[1];
-                else ++uses[0];
             }
+            if (most > 0) --n;                       // (the next item's first block has the number of the step without scores)
+            items += mine > 0;
         }
         if (!ok) sh->gave_up = 1;
-        for (int x = 0; x < kTlTiles; ++x)
-            if (uses[x] > 0) ptx::mbar_wait(&sh->q_raw[x], (uses[x] - 1) & 1);
-    } else if (warp >= 12) {
-        // ---------------- the MMAs ------------------------------------------------------------------------
-        // the whole warp walks the blocks, one elected lane issues; loops of few instructions (all roles' code together is what
-        // the instruction caches have to hold: unrolled and inlined freely it was 160 KB, and each item began with misses)
-        if (warp == 12) {
-            const bool issuer = elect_one();
-            const uint32_t id_s = idesc_f16(kTlRows, kTlBlock, false), id_o = idesc_f16(kTlRows, D, true);
-            // descriptors differ from these by multiples of 16 bytes in the address (their low 14 bits, which never carry)
-            const uint64_t d_q = ptx::smem_desc_sw128(s_u32, 16, 1024), d_k = ptx::smem_desc_sw128(k_u32, 16, 1024);
-            const uint64_t d_v = ptx::smem_desc_sw128(v_u32, S::kSlab, 1024);
-            bool ok = true;
-            uint32_t n = 0, items[kTlTiles] = {0, 0}, turns[kTlTiles] = {0, 0};     // blocks; each tile's items and blocks so far
-            TlItem t;
-#pragma unroll 1
-            for (uint32_t item = 0; ok && (ok = tl_take(sh, item, t)) && t.i >= 0; ++item) {
-                const int most = max(t.blocks[0], t.blocks[1]);
-                // step j: products of block j - 1 and scores of block j, tile by tile
-#pragma unroll 1
-                for (int j = 0; ok && most > 0 && j <= most; ++j, ++n) {
-                    // n: the line's number of block j
-                    bool have_k = false, have_v = false;
-#pragma unroll 1
-                    for (int x = 0; ok && x < kTlTiles; ++x) {
-                        const int mine = x ? t.blocks[1] : t.blocks[0];
-                        const uint32_t before = x ? items[1] : items[0], turn = x ? turns[1] : turns[0];
-                        if (j > 0 && j <= mine) {
-                            // the last item's output has been taken out of TMEM
-                            if (j == 1 && before > 0) ok = ptx::mbar_wait(&sh->o_empty[x], (before - 1) & 1);
-                            if (ok) ok = ptx::mbar_poll(&sh->p_full[x], turn & 1);
-                            if (ok && !have_v) ok = have_v = ptx::mbar_wait(&sh->v_full[(n - 1) & 1], ((n - 1) >> 1) & 1);
-                            if (!ok) break;
-                            ptx::tc_fence_after();
-                            if (issuer) {
-                                uint64_t v0 = d_v + ((n - 1) & 1) * (S::kOperand >> 4);
-                                uint32_t p0 = tmem + x * 128;
-#pragma unroll 1
-                                for (int k = 0; k < kTlBlock / 16; k += 4, v0 += 4 * 2048 >> 4, p0 += 32)
-#pragma unroll
-                                    for (int y = 0; y < 4; ++y)
-                                        umma_f16_ts(tmem + 256 + x * D, p0 + y * 8, v0 + y * (2048 >> 4), id_o, j - 1 + k + y > 0);
-                                if (j == mine) ptx::umma_commit(&sh->o_full[x]);
-                            }
-                            __syncwarp();
-                            if (x) ++turns[1];
-                            else ++turns[0];
-                        }
-                        if (j < mine) {
-                            if (j == 0) ok = ptx::mbar_wait(&sh->q_full[x], before & 1);
-                            if (ok && !have_k) ok = have_k = ptx::mbar_wait(&sh->k_full[n & 1], (n >> 1) & 1);
-                            if (!ok) break;
-                            ptx::tc_fence_after();
-                            if (issuer) {
-                                uint64_t q = d_q + x * (S::kOperand >> 4), k0 = d_k + (n & 1) * (S::kOperand >> 4);
-#pragma unroll 1
-                                for (int b = 0; b < S::kSlabs; ++b, q += S::kSlab >> 4, k0 += S::kSlab >> 4)
-#pragma unroll
-                                    for (int k = 0; k < 4; ++k) ptx::umma_bf16(tmem + x * 128, q + 2 * k, k0 + 2 * k, id_s, b + k > 0);
-                                ptx::umma_commit(&sh->s_full[x]);
-                                if (j + 1 == mine) ptx::umma_commit(&sh->q_empty[x]);
-                            }
-                            __syncwarp();
-                        }
-                    }
-                    if (ok && issuer) {
-                        if (j > 0) ptx::umma_commit(&sh->v_empty[(n - 1) & 1]);
-                        if (j < most) ptx::umma_commit(&sh->k_empty[n & 1]);
-                    }
-                    __syncwarp();
-                    if (j == most) break;            // (the next item's first block has this number)
-                }
-                items[0] += t.blocks[0] > 0;
-                items[1] += t.blocks[1] > 0;
-            }
-            if (!ok) sh->gave_up = 1;
-            // all MMAs done (also after a wait that gave up: the memory they use is about to be freed)
-            if (issuer) ptx::umma_commit(&sh->done);
-            __syncwarp();
-            if (!ptx::mbar_wait(&sh->done, 0)) sh->gave_up = 1;
-        }
+        // all MMAs done (also after a wait that gave up: the memory they use is about to be freed)
+        if (issuer) ptx::umma_commit(&sh->done);
+        __syncwarp();
+        if (!ptx::mbar_wait(&sh->done, 0)) sh->gave_up = 1;
+    }
     } else if (warp >= 8) {
+        regs_fewer<kTlCodeRegs>();
         // ---------------- codes to fp16 ---------------------------------------------------------------------
         // a thread's pieces: 16 codes of token 32 w + 8 q + lane / 4, piece lane % 4 of each slab, odd tokens the slabs in the other
         // order: eight neighbouring lanes read and write eight different places of 128 bytes
@@ -548,6 +528,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         }
         if (!ok) sh->gave_up = 1;
     } else {
+        regs_more<kTlSoftRegs>();
         // ---------------- a row per thread -------------------------------------------------------------------
         const int x = warp >> 2, r = tid & 127, jj = r / a.group, r_head = r - jj * a.group;   // a row's token of the tile, and its head
         const uint32_t q_tile = s_u32 + x * S::kOperand, lanes = (uint32_t)(warp & 3) << 21;
@@ -566,60 +547,67 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             const int warp_end = __shfl_sync(0xffffffffu, end, 0);      // the first row of the warp sees the fewest tokens
 #pragma unroll 1
             for (int j = 0; ok && j < blocks; ++j, ++turns) {
-                if (!(ok = ptx::mbar_poll(&sh->s_full[x], turns & 1))) break;
+                if (!(ok = ptx::mbar_wait(&sh->s_full[x], turns & 1))) break;
                 ptx::tc_fence_after();
                 const float4 *group = sh->group[(n + j) % kTlGroupRing];
                 const int left = end - j * kTlBlock; // tokens of the block that the row sees
                 const bool masked = (j + 1) * kTlBlock > warp_end;
-                float now = kAtNothing;              // the row's maximum (of s', with the values' scale)
-                uint32_t va[32], vb[32];
-                if (masked) {
-                    now = careful_top(group, factor, left, t_s);
-                } else {
-                    ptx::tmem_ld32(t_s, va);
-                    ptx::tmem_ld_wait();
-                    ptx::tmem_ld32(t_s + 32, vb);
-                    now = tile_top(va, group, factor, now);
-                    ptx::tmem_ld_wait();
-                    ptx::tmem_ld32(t_s + 64, va);
-                    now = tile_top(vb, group + 2, factor, now);
-                    ptx::tmem_ld_wait();
-                    ptx::tmem_ld32(t_s + 96, vb);
-                    now = tile_top(va, group + 4, factor, now);
-                    ptx::tmem_ld_wait();
-                    now = tile_top(vb, group + 6, factor, now);
-                }
-                if (__any_sync(0xffffffffu, now - top > kAtSlack)) {
-                    const float to = fmaxf(top, now), k = ex2(top - to);
-                    top = to;
-                    l *= k;
-                    if (j > 0) {
+                bool careful = masked;
+                // Weights against the maximum so far, in one pass; only where a row has one that is too large for fp16 by it (or nothing
+                // yet: the first block) its maximum is looked for first
+                for (bool first = j == 0 || masked;; first = true) {
+                    if (first) {
+                        float now = kAtNothing;      // the row's maximum (of s', with the values' scale)
+                        if (careful) {
+                            now = careful_top(group, factor, left, t_s);
+                        } else {
 #pragma unroll 1
-                        for (int c = 0; c < D / 16; ++c) {
-                            uint32_t o[16];
-                            ptx::tmem_ld16(t_o + c * 16, o);
-                            ptx::tmem_ld_wait();
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * k);
-                            tmem_st16(t_o + c * 16, o);
+                            for (int c = 0; c < 4; ++c) {
+                                uint32_t v[32];
+                                ptx::tmem_ld32(t_s + 32 * c, v);
+                                ptx::tmem_ld_wait();
+                                now = tile_top(v, group + 2 * c, factor, now);
+                            }
                         }
+                        const float to = fmaxf(top, now), k = ex2(top - to);
+                        top = to;
+                        l *= k;
+                        if (j > 0 && __any_sync(0xffffffffu, k < 1.f)) {
+#pragma unroll 1
+                            for (int c = 0; c < D / 16; ++c) {
+                                uint32_t o[16];
+                                ptx::tmem_ld16(t_o + c * 16, o);
+                                ptx::tmem_ld_wait();
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * k);
+                                tmem_st16(t_o + c * 16, o);
+                            }
+                        }
+                        careful = careful || __any_sync(0xffffffffu, fabsf(top) > kTlLarge);
                     }
-                }
-                if (masked || __any_sync(0xffffffffu, fabsf(top) > kTlLarge)) {
-                    careful_weights(group, factor, top, left, t_s, l);
-                } else {
+                    if (careful) {
+                        careful_weights(group, factor, top, left, t_s, l);
+                        break;
+                    }
+                    uint32_t va[32], vb[32], p[64];
+                    float most = -INFINITY, more = 0.f;
                     ptx::tmem_ld32(t_s, va);
                     ptx::tmem_ld_wait();
                     ptx::tmem_ld32(t_s + 32, vb);
-                    tile_weights(va, group, factor, top, t_s, l);
+                    tile_weights(va, group, factor, top, p, most, more);
                     ptx::tmem_ld_wait();
                     ptx::tmem_ld32(t_s + 64, va);
-                    tile_weights(vb, group + 2, factor, top, t_s + 16, l);
+                    tile_weights(vb, group + 2, factor, top, p + 16, most, more);
                     ptx::tmem_ld_wait();
                     ptx::tmem_ld32(t_s + 96, vb);
-                    tile_weights(va, group + 4, factor, top, t_s + 32, l);
+                    tile_weights(va, group + 4, factor, top, p + 32, most, more);
                     ptx::tmem_ld_wait();
-                    tile_weights(vb, group + 6, factor, top, t_s + 48, l);
+                    tile_weights(vb, group + 6, factor, top, p + 48, most, more);
+                    if (!first && __any_sync(0xffffffffu, most > kAtSlack)) continue;
+                    l += more;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_st16(t_s + 16 * c, *reinterpret_cast<uint32_t (*)[16]>(p + 16 * c));
+                    break;
                 }
                 tmem_st_wait();
                 ptx::tc_fence_before();
