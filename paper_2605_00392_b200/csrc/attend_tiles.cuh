@@ -2,12 +2,12 @@
 //
 // A CTA takes two tiles of rows of a request and kv head, each as many tokens as fit 128 rows with all their heads of that kv
 // head (a row per token and head, a token's heads beside each other), against blocks of 128 cached tokens:
-//   S = Q K^T   fp16 operands in shared memory, fp32 sums in TMEM
+//   S = Q K^T   bf16 operands in shared memory (queries as they are, codes exact), fp32 sums in TMEM
 //   P           fp16 weights, written over S in TMEM by the thread that owns the row
 //   O += P V    P from TMEM, V from shared memory, fp32 sums in TMEM
 // One CTA per SM takes items (two tiles) blockIdx.x, + gridDim.x, ...; what its warps do:
-//   0-3, 4-7  a row per thread of the first and second tile: softmax, output; and the next item's queries from bf16 to fp16, in place
-//   8-11      codes to fp16 in the swizzled operand layout (tiles of (token, 64 elements), K-major for the keys, MN-major for the values)
+//   0-3, 4-7  a row per thread of the first and second tile: softmax, output
+//   8-11      codes to bf16 (keys) and fp16 (values) in the swizzled operand layout (tiles of (token, 64 elements), K-major for the keys, MN-major for the values)
 //   12, 13    issue the MMAs of the first and second tile, in turns (one warp for both was the pace of the kernel)    14  bulk copies of codes    15  finds the items and fetches their queries, by TMA
 // S of a tile's next block is issued behind the PV of this one, whose P it overwrites.  The tiles take turns: one's PV and S, then the
 // other's, so that one's softmax runs beside the other's MMAs (left to themselves they fell into step, both softmaxes, then
@@ -27,7 +27,7 @@ constexpr int kTlTiles = 2;
 constexpr int kTlBlock = 128;                        // tokens of a block
 constexpr int kTlSoft = kTlTiles * kTlRows;
 constexpr int kTlThreads = kTlSoft + 128 + 128;     // (the last warp only makes it 128 registers a thread)
-constexpr int kTlSoftRegs = 184, kTlCodeRegs = 72, kTlOtherRegs = 72;    // registers of a thread: 2, 1, 1 of four warpgroups
+constexpr int kTlSoftRegs = 176, kTlCodeRegs = 64, kTlOtherRegs = 96;    // registers of a thread: 2, 1, 1 of four warpgroups
 static_assert(2 * kTlSoftRegs + kTlCodeRegs + kTlOtherRegs <= 4 * 128, "what the block was launched with");
 constexpr int kTlGroups = kTlBlock / 16;             // a page holds at least 16 tokens: scales are per 16
 
@@ -57,7 +57,7 @@ struct TlShared {
     uint64_t item_full[kTlItems], item_empty[kTlItems];
     uint64_t code_full[4], code_empty[4];            // keys of block 0, values of block 0, keys of block 1, ...
     uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
-    uint64_t q_raw[kTlTiles], q_full[kTlTiles], q_empty[kTlTiles], s_full[kTlTiles], p_full[kTlTiles], o_full[kTlTiles], o_empty[kTlTiles];
+    uint64_t q_full[kTlTiles], q_empty[kTlTiles], s_full[kTlTiles], p_full[kTlTiles], o_full[kTlTiles], o_empty[kTlTiles];
     uint64_t turn[kTlTiles], done;
     uint32_t tmem;
     volatile int gave_up;
@@ -116,14 +116,46 @@ __device__ inline void st_global_v8(void *p, const uint32_t *v)
 __device__ inline uint4 ld_shared_u4(uint32_t at)
 {
     uint4 v;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
     return v;
 }
-__device__ inline uint32_t max2_nan(uint32_t a, uint32_t b)
+// Four codes of a word, in order, as two pairs of bf16: 128 + the low seven bits is the bf16 number with those as its last bits, and 128
+// + 128 for the sign bit the one with that bit; their difference is the code.  (low, sign: 0x7f.., 0x80..; the other way round its negative.)
+__device__ inline void codes_to_bf16(uint32_t x, uint32_t low, uint32_t sign, uint32_t &lo, uint32_t &hi)
 {
-    uint32_t r;
-    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
+    constexpr uint32_t k128 = 0x43434343u;
+    const uint32_t a = x & low, b = x & sign;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(lo) : "r"(__byte_perm(a, k128, 0x4140)), "r"(__byte_perm(b, k128, 0x4140)));
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(hi) : "r"(__byte_perm(a, k128, 0x4342)), "r"(__byte_perm(b, k128, 0x4342)));
+}
+// A thread's pieces of a block's codes, to the operand: 16 codes of token 8 q + r, piece pc of each slab, odd tokens the slabs in the other
+// order: eight neighbouring lanes read and write eight different places of 128 bytes.
+template <int D, bool kValues>
+__device__ inline void tile_codes(uint32_t from, uint32_t to, int r, int pc, uint32_t low)
+{
+    constexpr int kSlabs = D / 64;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int b = 0; b < kSlabs; ++b) {
+            const int slab = b ^ (kSlabs > 1 ? r & 1 : 0);
+            const uint4 c = ld_shared_u4(from + 8 * q * D + (slab * 4 + pc) * 16);
+            uint4 lo, hi;
+            if (kValues) {
+                codes_to_half(c.x ^ 0x80808080u, lo.x, lo.y);
+                codes_to_half(c.y ^ 0x80808080u, lo.z, lo.w);
+                codes_to_half(c.z ^ 0x80808080u, hi.x, hi.y);
+                codes_to_half(c.w ^ 0x80808080u, hi.z, hi.w);
+            } else {
+                codes_to_bf16(c.x, low, ~low, lo.x, lo.y);
+                codes_to_bf16(c.y, low, ~low, lo.z, lo.w);
+                codes_to_bf16(c.z, low, ~low, hi.x, hi.y);
+                codes_to_bf16(c.w, low, ~low, hi.z, hi.w);
+            }
+            const uint32_t line = to + slab * 16384 + 8 * q * 128;
+            ptx::st_shared_v4(line + (((2 * pc) ^ r) << 4), lo);          // (32 w + 8 q + r) & 7 = r
+            ptx::st_shared_v4(line + (((2 * pc + 1) ^ r) << 4), hi);
+        }
 }
 // Two fp32 at a time.
 __device__ inline uint64_t pack2(float a, float b)
@@ -195,45 +227,51 @@ __device__ inline void tile_weights(const uint32_t (&v)[32], const float4 *group
 }
 // The same where tokens from `left` on are not seen, or scores are so large that their own rounding matters: it is what the maximum
 // went through, so they go through it too before the maximum is taken off.  Loops of few instructions, from TMEM again.
-__device__ inline float careful_top(const float4 *group, float factor, int left, uint32_t t_s)
+__device__ inline float careful_top(const float4 *group, float factor, int left, int seen, uint32_t t_s)
 {
     float now = kAtNothing;
 #pragma unroll 1
-    for (int c = 0; c < kTlGroups; ++c, left -= 16) {
-        uint32_t v[16];
-        ptx::tmem_ld16(t_s + c * 16, v);
-        ptx::tmem_ld_wait();
-        float s[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = e < left ? __uint_as_float(v[e]) : -INFINITY;
-        const float4 g = group[c];
-        now = fmaxf(now, fmaf(max16(s), factor * g.x, g.y));
-    }
-    return now;
-}
-__device__ inline void careful_weights(const float4 *group, float factor, float top, int left, uint32_t t_s, float &l)
-{
-#pragma unroll 1
-    for (int c = 0; c < kTlBlock / 32; ++c) {
-        uint32_t v[32], p[16];
+    for (int c = 0; 32 * c < seen; ++c, left -= 32) {
+        uint32_t v[32];
         ptx::tmem_ld32(t_s + c * 32, v);
         ptx::tmem_ld_wait();
 #pragma unroll
-        for (int h = 0; h < 2; ++h, left -= 16) {
-            const float4 g = group[2 * c + h];
-            const float k = factor * g.x;
-            float sum = 0.f;
+        for (int h = 0; h < 2; ++h) {
+            float s[16];
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-                float w0 = ex2(fmaf(__uint_as_float(v[16 * h + e]), k, g.y) - top);
-                float w1 = ex2(fmaf(__uint_as_float(v[16 * h + e + 1]), k, g.y) - top);
-                w0 = e < left ? w0 : 0.f;
-                w1 = e + 1 < left ? w1 : 0.f;
-                sum += w0 + w1;
-                p[8 * h + e / 2] = pack_half(w0, w1);
+            for (int e = 0; e < 16; ++e) s[e] = 16 * h + e < left ? __uint_as_float(v[16 * h + e]) : -INFINITY;
+            const float4 g = group[2 * c + h];
+            now = fmaxf(now, fmaf(max16(s), factor * g.x, g.y));
+        }
+    }
+    return now;
+}
+__device__ inline void careful_weights(const float4 *group, float factor, float top, int left, int seen, uint32_t t_s, float &l)
+{
+#pragma unroll 1
+    for (int c = 0; c < kTlBlock / 32; ++c, left -= 32) {
+        uint32_t v[32], p[16];
+        if (32 * c < seen) {
+            ptx::tmem_ld32(t_s + c * 32, v);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float4 g = group[2 * c + h];
+                const float k = factor * g.x;
+                float w[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e] = ex2(fmaf(__uint_as_float(v[16 * h + e]), k, g.y) - top);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e] = 16 * h + e < left ? w[e] : 0.f;
+                const float sum = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])) + (((w[8] + w[9]) + (w[10] + w[11])) + ((w[12] + w[13]) + (w[14] + w[15])));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[8 * h + e] = pack_half(w[2 * e], w[2 * e + 1]);
+                // weights of 0 add nothing, whatever the block's scale is (of a page that the row does not see)
+                if (sum != 0.f) l = fmaf(sum, g.z, l);
             }
-            // weights of 0 add nothing, whatever the block's scale is (of a page that the row does not see)
-            if (sum != 0.f) l = fmaf(sum, g.z, l);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) p[e] = 0u;
         }
         tmem_st16(t_s + c * 16, p);
     }
@@ -265,8 +303,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             ptx::mbar_init(&sh->v_empty[s], kTlTiles);
         }
         for (int x = 0; x < kTlTiles; ++x) {
-            ptx::mbar_init(&sh->q_raw[x], 1);
-            ptx::mbar_init(&sh->q_full[x], kTlRows);
+            ptx::mbar_init(&sh->q_full[x], 1);
             ptx::mbar_init(&sh->q_empty[x], 1);
             ptx::mbar_init(&sh->s_full[x], 1);
             ptx::mbar_init(&sh->p_full[x], kTlRows);
@@ -299,7 +336,9 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         // ---------------- the work: items blockIdx.x, + gridDim.x, ... that have rows; their queries, as they are, in the operand's
         // layout already
         const int per = a.batch * a.c.kv_heads, all = row_blocks * per;
-        int at = blockIdx.x;
+        auto number = [&](int round) { return round * (int)gridDim.x + (int)(round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x); };
+        const int rounds = (all + (int)gridDim.x - 1) / (int)gridDim.x;
+        int at = 0;
         bool ok = true;
         uint32_t uses[kTlTiles] = {0, 0};
 #pragma unroll 1
@@ -308,10 +347,10 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             t.i = -1;
             // 32 of the numbers at a time, one per lane (bounds that are far above the requests' lengths leave most of them empty)
 #pragma unroll 1
-            for (; at < all; at += 32 * gridDim.x) {
-                const int mine = at + lane * gridDim.x;
+            for (; at < rounds; at += 32) {
+                const int mine = number(at + lane);
                 bool has = false;
-                if (mine < all) {
+                if (at + lane < rounds && mine < all) {
                     // the last rows of every request first: with a causal mask they have the most to do
                     const int rest = mine % per;
                     t.i = rest / a.c.kv_heads;
@@ -322,7 +361,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                 const uint32_t found = __ballot_sync(0xffffffffu, has);
                 if (found) {
                     const int from = __ffs(found) - 1;
-                    at += (from + 1) * gridDim.x;
+                    at += from + 1;
                     t.i = __shfl_sync(0xffffffffu, t.i, from);
                     t.head = __shfl_sync(0xffffffffu, t.head, from);
                     t.j0 = __shfl_sync(0xffffffffu, t.j0, from);
@@ -350,9 +389,9 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                 if (!ok || t.blocks[x] == 0) continue;
                 if (uses[x] > 0) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&sh->q_empty[x], (uses[x] - 1) & 1));
                 if (ok && lane == 0) {
-                    ptx::mbar_arrive_expect_tx(&sh->q_raw[x], (uint32_t)(S::kSlabs * tile_tokens * a.group * 128));
+                    ptx::mbar_arrive_expect_tx(&sh->q_full[x], (uint32_t)(S::kSlabs * tile_tokens * a.group * 128));
                     for (int b = 0; b < S::kSlabs; ++b)
-                        ptx::tma_load_3d(s_u32 + x * S::kOperand + b * S::kSlab, &map_q, &sh->q_raw[x], b * 64, t.head * a.group,
+                        ptx::tma_load_3d(s_u32 + x * S::kOperand + b * S::kSlab, &map_q, &sh->q_full[x], b * 64, t.head * a.group,
                                          t.row0 + t.j0 + x * tile_tokens);
                 }
                 __syncwarp();
@@ -363,7 +402,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         // no copy is left on its way into memory that this CTA gives back
 #pragma unroll
         for (int x = 0; x < kTlTiles; ++x)
-            if (uses[x] > 0) ptx::mbar_wait(&sh->q_raw[x], (uses[x] - 1) & 1);
+            if (uses[x] > 0) ptx::mbar_wait(&sh->q_full[x], (uses[x] - 1) & 1);
     } else if (warp == 14) {
         // ---------------- codes of the items' blocks, and their scales ----------------------------------------
         const int per_page = min(a.c.page_size, kTlBlock), copies = kTlBlock / per_page;   // a page of a head is one piece of memory
@@ -411,7 +450,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         // the whole warp walks the blocks, one elected lane issues
         const int x = warp - 12;
         const bool issuer = elect_one();
-        const uint32_t id_s = idesc_f16(kTlRows, kTlBlock, false), id_o = idesc_f16(kTlRows, D, true);
+        const uint32_t id_s = ptx::idesc_bf16(kTlRows, kTlBlock, false, false), id_o = idesc_f16(kTlRows, D, true);
         const uint32_t t_s = tmem + x * 128, t_o = tmem + 256 + x * D;
         // descriptors differ from these by multiples of 16 bytes in the address (their low 14 bits, which never carry)
         const uint64_t d_q = ptx::smem_desc_sw128(s_u32 + x * S::kOperand, 16, 1024), d_k = ptx::smem_desc_sw128(k_u32, 16, 1024);
@@ -479,10 +518,9 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     }
     } else if (warp >= 8) {
         regs_fewer<kTlCodeRegs>();
-        // ---------------- codes to fp16 ---------------------------------------------------------------------
-        // a thread's pieces: 16 codes of token 32 w + 8 q + lane / 4, piece lane % 4 of each slab, odd tokens the slabs in the other
-        // order: eight neighbouring lanes read and write eight different places of 128 bytes
+        // ---------------- codes to bf16 and fp16 ---------------------------------------------------------------------
         const int w = warp - 8, r = lane >> 2, pc = lane & 3;
+        const uint32_t low = a.scale_log2 < 0.f ? 0x80808080u : 0x7f7f7f7fu;       // (a negative scale: negative keys)
         TlItem t;
         bool ok = true;
         uint32_t n = 0, copy = 0;
@@ -495,32 +533,12 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                 const uint32_t slot = copy % S::kSlots, s = n & 1;
                 ok = ptx::mbar_wait(&sh->code_full[slot], copy / S::kSlots & 1);
                 if (!ok) break;
-                uint4 x[4 * S::kSlabs];
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int b = 0; b < S::kSlabs; ++b)
-                        x[q * S::kSlabs + b] = ld_shared_u4(code_u32 + slot * S::kSlot + (32 * w + 8 * q + r) * D + ((b ^ (S::kSlabs > 1 ? r & 1 : 0)) * 4 + pc) * 16);
-                ptx::mbar_arrive(&sh->code_empty[slot]);
                 if (n >= 2) ok = ptx::mbar_wait(values ? &sh->v_empty[s] : &sh->k_empty[s], ((n >> 1) - 1) & 1);
                 if (!ok) break;
-                const uint32_t to = (values ? v_u32 : k_u32) + s * S::kOperand;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int tk = 32 * w + 8 * q + r;
-#pragma unroll
-                    for (int b = 0; b < S::kSlabs; ++b) {
-                        const uint4 c = x[q * S::kSlabs + b];
-                        uint4 lo, hi;
-                        codes_to_half(c.x ^ 0x80808080u, lo.x, lo.y);
-                        codes_to_half(c.y ^ 0x80808080u, lo.z, lo.w);
-                        codes_to_half(c.z ^ 0x80808080u, hi.x, hi.y);
-                        codes_to_half(c.w ^ 0x80808080u, hi.z, hi.w);
-                        const uint32_t line = to + (b ^ (S::kSlabs > 1 ? r & 1 : 0)) * S::kSlab + tk * 128;
-                        ptx::st_shared_v4(line + (((2 * pc) ^ (tk & 7)) << 4), lo);
-                        ptx::st_shared_v4(line + (((2 * pc + 1) ^ (tk & 7)) << 4), hi);
-                    }
-                }
+                const uint32_t from = code_u32 + slot * S::kSlot + (32 * w + r) * D, to = (values ? v_u32 : k_u32) + s * S::kOperand + (32 * w + r) * 128;
+                if (values) tile_codes<D, true>(from, to, r, pc, low);
+                else tile_codes<D, false>(from, to, r, pc, low);
+                ptx::mbar_arrive(&sh->code_empty[slot]);
                 ptx::fence_proxy_async_smem();
                 ptx::mbar_arrive(values ? &sh->v_full[s] : &sh->k_full[s]);
                 n += values;
@@ -531,20 +549,18 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         regs_more<kTlSoftRegs>();
         // ---------------- a row per thread -------------------------------------------------------------------
         const int x = warp >> 2, r = tid & 127, jj = r / a.group, r_head = r - jj * a.group;   // a row's token of the tile, and its head
-        const uint32_t q_tile = s_u32 + x * S::kOperand, lanes = (uint32_t)(warp & 3) << 21;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
         const uint32_t t_s = tmem + lanes + x * 128, t_o = tmem + lanes + 256 + x * D;
-        constexpr int kLanes = D / 8;                // lanes of a row when a warp takes whole rows, 16 bytes a lane
-        constexpr int kRowsAt = 32 / kLanes;
         bool ok = true;
-        uint32_t n = 0, turns = 0, items = 0, items_q = 0;     // blocks; this tile's blocks, items and queries so far
+        uint32_t n = 0, turns = 0, items = 0;        // blocks; this tile's blocks and items so far
         // the item in work: what of it outlives the look at the next one
         int mine = -1, end = 0, blocks = 0, most = 0;
-        float factor = 0.f;                          // of the row's scores
+        const float factor = fabsf(a.scale_log2);    // (a negative scale is in the keys: the largest sum is the largest score)
         bool has = false, bad = false;
 #pragma unroll 1
         for (uint32_t item = 0;; ++item) {
             float top = kAtNothing, l = 0.f;
-            const int warp_end = __shfl_sync(0xffffffffu, end, 0);      // the first row of the warp sees the fewest tokens
+            const int warp_most = __shfl_sync(0xffffffffu, end, 31); const int warp_end = __shfl_sync(0xffffffffu, end, 0);      // the first row of the warp sees the fewest tokens
 #pragma unroll 1
             for (int j = 0; ok && j < blocks; ++j, ++turns) {
                 if (!(ok = ptx::mbar_wait(&sh->s_full[x], turns & 1))) break;
@@ -552,6 +568,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                 const float4 *group = sh->group[(n + j) % kTlGroupRing];
                 const int left = end - j * kTlBlock; // tokens of the block that the row sees
                 const bool masked = (j + 1) * kTlBlock > warp_end;
+                const int seen = min(warp_most - j * kTlBlock, kTlBlock);
                 bool careful = masked;
                 // Weights against the maximum so far, in one pass; only where a row has one that is too large for fp16 by it (or nothing
                 // yet: the first block) its maximum is looked for first
@@ -559,14 +576,16 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                     if (first) {
                         float now = kAtNothing;      // the row's maximum (of s', with the values' scale)
                         if (careful) {
-                            now = careful_top(group, factor, left, t_s);
+                            now = careful_top(group, factor, left, seen, t_s);
                         } else {
 #pragma unroll 1
-                            for (int c = 0; c < 4; ++c) {
-                                uint32_t v[32];
-                                ptx::tmem_ld32(t_s + 32 * c, v);
+                            for (int c = 0; c < 4; c += 2) {
+                                uint32_t va[32], vb[32];
+                                ptx::tmem_ld32(t_s + 32 * c, va);
+                                ptx::tmem_ld32(t_s + 32 * c + 32, vb);
                                 ptx::tmem_ld_wait();
-                                now = tile_top(v, group + 2 * c, factor, now);
+                                now = tile_top(va, group + 2 * c, factor, now);
+                                now = tile_top(vb, group + 2 * c + 2, factor, now);
                             }
                         }
                         const float to = fmaxf(top, now), k = ex2(top - to);
@@ -586,7 +605,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                         careful = careful || __any_sync(0xffffffffu, fabsf(top) > kTlLarge);
                     }
                     if (careful) {
-                        careful_weights(group, factor, top, left, t_s, l);
+                        careful_weights(group, factor, top, left, seen, t_s, l);
                         break;
                     }
                     uint32_t va[32], vb[32], p[64];
@@ -614,8 +633,6 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                 ptx::mbar_arrive(&sh->p_full[x]);
             }
             n += most;
-            // ---- the next item's queries, while this one's last products run: scaled, to fp16 in the operand's layout, in place.  (The
-            // tile's queries before are done with: the last scores of theirs have come.)
             TlItem next;
             if (!tl_take(sh, item, next)) {
                 ok = false;
@@ -623,53 +640,12 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                 next.i = -1;
             }
             int mine_next = -1, end_next = 0;
-            float factor_next = 0.f;
             if (next.i >= 0) {
                 const int j_row = next.j0 + x * tile_tokens + jj;
                 if (jj < tile_tokens && j_row < next.n) mine_next = (next.row0 + j_row) * a.q_heads + next.head * a.group + r_head;
                 end_next = a.causal ? next.len - next.n + 1 + min(j_row, next.n - 1) : next.len;
             }
             const int blocks_next = next.i < 0 ? 0 : x ? next.blocks[1] : next.blocks[0];
-            if (ok && blocks_next > 0) {
-                if (!(ok = ptx::mbar_wait(&sh->q_raw[x], items_q & 1))) sh->gave_up = 1;
-                ++items_q;
-                // a warp's step: 16 lanes (D = 64: 8) a row
-#pragma unroll 1
-                for (int e = 0; e < 32; e += 4 * kRowsAt) {
-                    uint4 raw[4];
-                    const int ch = lane % kLanes;
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const int rr = e + g * kRowsAt + lane / kLanes;
-                        const bool real = __shfl_sync(0xffffffffu, mine_next, rr) >= 0;
-                        raw[g] = ld_shared_u4(q_tile + (ch >> 3) * S::kSlab + ((r & ~31) + rr) * 128 + (((ch & 7) ^ (rr & 7)) << 4));
-                        if (!real) raw[g] = make_uint4(0u, 0u, 0u, 0u);
-                    }
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        // the row's largest |q|, on the bf16 bits: of 8 elements, then over the row's lanes
-                        uint32_t w = max2_nan(max2_nan(raw[g].x & 0x7fff7fffu, raw[g].y & 0x7fff7fffu), max2_nan(raw[g].z & 0x7fff7fffu, raw[g].w & 0x7fff7fffu));
-                        w = max2_nan(w, w >> 16);
-#pragma unroll
-                        for (int o = kLanes / 2; o > 0; o >>= 1) w = max2_nan(w, __shfl_xor_sync(0xffffffffu, w, o));
-                        float f[8], factor_q;
-                        float unit = query_scale(__uint_as_float(w << 16), a.scale_log2, factor_q);
-                        if (factor_q < 0.f) {        // the scores' factor is positive: the largest sum is the largest score
-                            factor_q = -factor_q;
-                            unit = -unit;
-                        }
-                        Elem<__nv_bfloat16>::unpack(raw[g], f);
-                        const int rr = (r & ~31) + e + g * kRowsAt + lane / kLanes;
-                        factor_q = __shfl_sync(0xffffffffu, factor_q, lane % kRowsAt * kLanes);    // to the row's own thread
-                        if (lane / kRowsAt == e / kRowsAt + g) factor_next = factor_q;
-                        ptx::st_shared_v4(q_tile + (ch >> 3) * S::kSlab + rr * 128 + (((ch & 7) ^ (rr & 7)) << 4),
-                                          make_uint4(pack_half(f[0] * unit, f[1] * unit), pack_half(f[2] * unit, f[3] * unit),
-                                                     pack_half(f[4] * unit, f[5] * unit), pack_half(f[6] * unit, f[7] * unit)));
-                    }
-                }
-                ptx::fence_proxy_async_smem();
-                ptx::mbar_arrive(&sh->q_full[x]);
-            }
             // ---- out
             if (has) {
                 const bool any = blocks > 0;
@@ -709,7 +685,6 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             bad = next.len < 0;
             mine = mine_next;
             end = end_next;
-            factor = factor_next;
             blocks = blocks_next;
             most = max(next.blocks[0], next.blocks[1]);
         }
