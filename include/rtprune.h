@@ -337,7 +337,7 @@ rtprune_status_t rtprune_test_density_expired(void *cuda_stream, const uint8_t *
 typedef struct {
     int8_t *k, *v;            /* DEVICE [num_pages][kv_heads][page_size][head_dim] codes, 16-byte aligned */
     float *k_scale, *v_scale; /* DEVICE [num_pages][kv_heads]                                             */
-    int64_t num_pages;        /* num_pages * page_size <= 2^31 - 1                                        */
+    int64_t num_pages;        /* num_pages * kv_heads * page_size <= 2^31 - 1                             */
     int32_t page_size;        /* 16, 32, 64 or 128                                                        */
     int32_t kv_heads;         /* at most 1024                                                             */
     int32_t head_dim;         /* 64 or 128                                                                */

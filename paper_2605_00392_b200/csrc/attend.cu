@@ -46,6 +46,34 @@ static int device_sms()
     return sms;
 }
 
+// A tensor of rows of `dims` elements for TMA, boxes of `box`; at most three dimensions.
+static bool tensor_map(CUtensorMap *map, CUtensorMapDataType type, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides,
+                       const cuuint32_t *box, CUtensorMapSwizzle swizzle)
+{
+    typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                      const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                      CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static std::atomic<void *> encode{nullptr};       // the driver's entry point, looked up once
+    void *fn = encode.load(std::memory_order_relaxed);
+    if (!fn) {
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            return false;
+        encode.store(fn, std::memory_order_relaxed);
+    }
+    const cuuint32_t unit[3] = {1, 1, 1};
+    return ((EncodeTiledFn)fn)(map, type, (cuuint32_t)rank, const_cast<void *>(base), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                               swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// The queries (element, head, row); boxes of 64 elements of `heads` heads of `tokens` rows.
+static bool queries_map(CUtensorMap *map, const AttendArgs &a, int heads, int tokens)
+{
+    const cuuint64_t dims[3] = {(cuuint64_t)a.c.dim, (cuuint64_t)a.q_heads, (cuuint64_t)a.rows};
+    const cuuint64_t strides[2] = {(cuuint64_t)a.c.dim * 2, (cuuint64_t)a.q_stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)heads, (cuuint32_t)tokens};
+    return tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.q, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
 template <int D>
 static cudaError_t launch_rows(const AttendArgs &a, int ctas, uint8_t *ws, cudaStream_t st)
 {
@@ -65,29 +93,6 @@ static int64_t tile_row_blocks(const AttendArgs &a)
 {
     const int tokens = kTlTiles * (kTlRows / a.group);
     return (std::min(a.max_q_len, a.rows) + tokens - 1) / tokens;
-}
-
-// The queries as a tensor (element, head, row); boxes of 64 elements of `heads` heads of `tokens` rows, 128-byte swizzle.
-static bool queries_map(CUtensorMap *map, const AttendArgs &a, int heads, int tokens)
-{
-    typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                      const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                      CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static std::atomic<void *> encode{nullptr};       // the driver's entry point, looked up once
-    void *fn = encode.load(std::memory_order_relaxed);
-    if (!fn) {
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess)
-            return false;
-        encode.store(fn, std::memory_order_relaxed);
-    }
-    const cuuint64_t dims[3] = {(cuuint64_t)a.c.dim, (cuuint64_t)a.q_heads, (cuuint64_t)a.rows};
-    const cuuint64_t strides[2] = {(cuuint64_t)a.c.dim * 2, (cuuint64_t)a.q_stride * 2};
-    const cuuint32_t box[3] = {64, (cuuint32_t)heads, (cuuint32_t)tokens}, unit[3] = {1, 1, 1};
-    return ((EncodeTiledFn)fn)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16 *>(a.q), dims, strides, box, unit,
-                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int D>

@@ -6,11 +6,13 @@
 // time per SM and 0.02 of mma), and its fragments come straight out of 16-byte loads because both contractions may run in any order:
 //   scores  a lane takes 32 (D = 64: 16) neighbouring elements of a token's key; the queries' fragments are laid out to match
 //   values  a lane takes 16 (8) neighbouring columns of four tokens: n-tile j of the output is column 16 g + j of each lane group g
-// Codes come through a warp's own ring of cp.async stages in shared memory, 16-byte pieces swizzled by row so that both ways of reading
-// are free of conflicts; the scales of a stage's block come with it.
+// Codes come by 16-byte cp.async into a ring of steps in shared memory, the pieces swizzled by row so that both ways of reading find them in
+// different banks; a fifth warp fetches them, with the scales of their blocks, and walks the tables: the four others have nothing but
+// the arithmetic, about 300 instructions for 16 tokens, and that is what HBM is kept waiting by (with the fetching in the same warps it
+// was 540, and 4.7 TB/s).
 //
 // The work, all (request, kv head, tile of rows) with their blocks of 64 tokens, is one line that is cut into equal runs, one per CTA
-// (three to an SM), whatever the requests' lengths: each CTA sums up the batch for itself and finds its place.  A tile that a cut goes through is
+// (two to an SM), whatever the requests' lengths: each CTA sums up the batch for itself and finds its place.  A tile that a cut goes through is
 // left in parts (fp32 sums, m', l) that attend_join_kernel puts together in the order of the line, so results do not depend on timing.
 // The ring runs across tiles: the next one's codes are on their way while this one's warps are added up.
 #pragma once
@@ -18,23 +20,23 @@
 
 namespace rtp {
 
-constexpr int kArWarps = 4;
-constexpr int kArThreads = 32 * kArWarps;
+constexpr int kArWarps = 4;                          // that compute; one more fetches
+constexpr int kArThreads = 32 * (kArWarps + 1);
 constexpr int kArBlock = 16 * kArWarps;              // tokens of a step
-constexpr int kArPerSm = 3;                          // CTAs of an SM
+constexpr int kArPerSm = 2;                          // CTAs of an SM (three leave a thread 128 registers, which spill)
 constexpr int kArMostCtas = kArPerSm * 160;          // what the workspace is sized for (a B200 has 148 SMs)
 constexpr int kArRows = 16;
 constexpr int kArLeast = 4;                          // blocks of a run at least
 
 template <int D> struct ArShape {
-    static constexpr int kStages = D == 128 ? 3 : 6;
-    static constexpr int kTile = 16 * D;             // bytes of a warp's keys (or values) of a stage
+    static constexpr int kStages = D == 128 ? 5 : 10;
+    static constexpr int kBytes = kArBlock * D;      // keys (or values) of a step
     static constexpr int kSteps = D / 16;            // mma steps of a score
     static constexpr int kNt = D / 8;                // n-tiles of the output
-    static constexpr int kRing = kArWarps * kStages * 2 * kTile;
+    static constexpr int kRing = kStages * 2 * kBytes;
     static constexpr int kFrag = kSteps * 32 * 16;   // the queries' fragments
     static constexpr int kJoin = (kArWarps / 2) * 32 * kNt * 16;   // accumulators of half the warps
-    static constexpr int kSmem = kRing + kFrag + kJoin + kArWarps * kStages * 8;
+    static constexpr int kSmem = kRing + kFrag + kJoin + 1024 /*alignment*/;
 };
 
 // A place in the line of work.
@@ -52,10 +54,11 @@ struct ArPlace {
             blocks = max(1, (len + kArBlock - 1) / kArBlock);
         }
     }
-    // (the line ends before the batch does: the caller counts)
-    __device__ void next(const AttendArgs &a)
+    // `steps` blocks on, within the tile or to the next one's first (the line ends before the batch does: the caller counts)
+    __device__ void next(const AttendArgs &a, int steps)
     {
-        if (++block < blocks) return;
+        block += steps;
+        if (block < blocks) return;
         block = 0;
         if (++tile < tiles) return;
         tile = 0;
@@ -75,7 +78,7 @@ __device__ inline int64_t ar_units(const AttendArgs &a, int i)
 // Where CTA `blockIdx.x` of the line begins, and how many blocks it takes (0: none).
 __device__ inline int ar_find(const AttendArgs &a, ArPlace &at, int &chunk)
 {
-    __shared__ int64_t warp_units[kArWarps], found_before;
+    __shared__ int64_t warp_units[kArWarps + 1], found_before;
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (a.batch + kArThreads - 1) / kArThreads, i0 = min(tid * per, a.batch), i1 = min(i0 + per, a.batch);
@@ -91,7 +94,7 @@ __device__ inline int ar_find(const AttendArgs &a, ArPlace &at, int &chunk)
     __syncthreads();
     int64_t total = 0, before = upto - mine;
 #pragma unroll
-    for (int w = 0; w < kArWarps; ++w) {
+    for (int w = 0; w <= kArWarps; ++w) {
         if (w < warp) before += warp_units[w];
         total += warp_units[w];
     }
@@ -138,12 +141,16 @@ __device__ inline float2 lds_f2(uint32_t at)
     asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at));
     return v;
 }
-__device__ inline void cp_async_4(uint32_t dst_smem, const void *src)
+__device__ inline float4 lds_f4(uint32_t at)
 {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst_smem), "l"(src) : "memory");
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
+    return v;
 }
+// The four warps that compute, among themselves.
+__device__ inline void ar_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kArWarps) : "memory"); }
 
-// Place of 16-byte piece `ch` of row t of a tile.
+// Place of 16-byte piece `ch` of row t of a step (rows of a warp's 16 tokens are 16 neighbouring rows).
 template <int D> __device__ inline uint32_t ar_piece(int t, int ch)
 {
     if (D == 128) return (uint32_t)(t * 128 + ((ch ^ (t & 7)) << 4));
@@ -156,65 +163,93 @@ template <int D> __device__ inline uint32_t ar_piece(int t, int ch)
 // (first row of the request, kv head, the tile's first row | its rows << 26, CTAs that it goes through; 0: there is none).
 template <int D>
 __global__ void __launch_bounds__(kArThreads, kArPerSm)
-attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ part, float2 *__restrict__ part_ml,
-                   int4 *__restrict__ join)
+attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ part, float2 *__restrict__ part_ml, int4 *__restrict__ join)
 {
     using S = ArShape<D>;
-    extern __shared__ __align__(128) uint8_t sm[];
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ float row_factor[kArRows];
     __shared__ float2 row_ml[kArWarps][kArRows];
+    __shared__ float4 scales[S::kStages][kArWarps];  // ks, log2 vs, 1 / vs of each warp's 16 tokens
+    __shared__ uint64_t full[S::kStages], empty[S::kStages];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-    const uint32_t ring = ptx::smem_u32(sm) + warp * S::kStages * 2 * S::kTile;
-    const uint32_t frag = ptx::smem_u32(sm) + S::kRing;
-    const uint32_t scales = frag + S::kFrag + S::kJoin + warp * S::kStages * 8;
-    float4 *joined = reinterpret_cast<float4 *>(sm + S::kRing + S::kFrag);
+    const uint32_t ring = ptx::smem_u32(sm), frag = ring + S::kRing, scales_u32 = ptx::smem_u32(scales);
+    const uint32_t joined = frag + S::kFrag + lane * 16;
+    if (tid == 0) {
+        for (int s = 0; s < S::kStages; ++s) {
+            ptx::mbar_init(&full[s], 33);            // every lane's copies, and the scales
+            ptx::mbar_init(&empty[s], kArWarps);
+        }
+        ptx::fence_mbar_init();
+    }
     ptx::grid_dep_launch();
     ptx::grid_dep_wait();
-    ArPlace at, ahead;
+    ArPlace at;
     int chunk;
-    const int todo = ar_find(a, at, chunk);
+    const int todo = ar_find(a, at, chunk);          // (its barriers order the initialisation too)
     if (todo == 0) {
         if (tid == 0) join[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
-    ahead = at;
 
-    // the next block's codes of this warp (16 tokens) on their way into stage s
-    int ahead_left = todo, stage_in = 0;
-    auto fetch = [&]() {
-        if (ahead_left > 0) {
-            const int t0 = ahead.block * kArBlock + warp * 16;
-            if (t0 < ahead.len) {
-                const int page = attend_page(a, ahead.i, t0);
-                const int64_t block = (int64_t)max(page, 0) * a.c.kv_heads + ahead.head;
-                const int64_t from = (block * a.c.page_size + (t0 & (a.c.page_size - 1))) * D;
-                const uint32_t to = ring + stage_in * 2 * S::kTile;
-#pragma unroll
-                for (int p = 0; p < D / 32; ++p) {
-                    const int piece = lane + 32 * p, t = piece / (D / 16), ch = piece % (D / 16);
-                    ptx::cp_async_16(to + ar_piece<D>(t, ch), a.c.k + from + piece * 16, 16);
-                    ptx::cp_async_16(to + S::kTile + ar_piece<D>(t, ch), a.c.v + from + piece * 16, 16);
-                }
-                if (lane < 2) {
-                    const uint32_t s_to = scales + stage_in * 8 + lane * 4;
-                    if (page >= 0) cp_async_4(s_to, (lane ? a.c.v_scale : a.c.k_scale) + block);
-                    else asm volatile("st.shared.b32 [%0], %1;" ::"r"(s_to), "r"(0x7fc00000u) : "memory");
-                }
+    if (warp == kArWarps) {
+        // ---------------- codes and scales: a step ahead with the tables ---------------------------------------
+        const float nan = __uint_as_float(0x7fc00000u);
+        uint32_t n = 0;
+        // of the step that is fetched, for the 16 tokens of warp lane / 8: their block (-1: none), and the codes' place in it
+        int block = -1, slot = 0;
+#pragma unroll 1
+        for (int look = 0; look <= todo; ++look) {
+            int next_block = -1, next_slot = 0;
+            if (look < todo) {
+                const int t = at.block * kArBlock + (lane >> 3) * 16;
+                const int page = t < at.len ? attend_page(a, at.i, t) : -1;
+                next_block = page < 0 ? -1 : page * a.c.kv_heads + at.head;
+                next_slot = t & (a.c.page_size - 1);
+                at.next(a, 1);
             }
-            --ahead_left;
-            ahead.next(a);
+            if (look > 0) {
+                const uint32_t s = n % S::kStages, turn = n / S::kStages, to = ring + s * 2 * S::kBytes;
+                const float ks = block < 0 ? nan : __ldg(a.c.k_scale + block), vs = block < 0 ? nan : __ldg(a.c.v_scale + block);
+                bool ok = true;
+                if (turn > 0) ok = ptx::mbar_wait(&empty[s], (turn - 1) & 1);
+                if (!__all_sync(0xffffffffu, ok)) break;
+                const int64_t from = ((int64_t)max(block, 0) * a.c.page_size + slot) * D;
+#pragma unroll
+                for (int w = 0; w < kArWarps; ++w) {
+                    if (__shfl_sync(0xffffffffu, block, 8 * w) < 0) continue;
+                    const int64_t base = __shfl_sync(0xffffffffu, from, 8 * w);
+#pragma unroll
+                    for (int p = 0; p < D / 32; ++p) {
+                        const int piece = lane + 32 * p, t = piece / (D / 16), ch = piece % (D / 16);
+                        const uint32_t place = to + ar_piece<D>(16 * w + t, ch);
+                        ptx::cp_async_16(place, a.c.k + base + piece * 16, 16);
+                        ptx::cp_async_16(place + S::kBytes, a.c.v + base + piece * 16, 16);
+                    }
+                }
+                ptx::cp_async_arrive(&full[s]);
+                float lv, inv;
+                value_scale(vs, lv, inv);
+                if ((lane & 7) == 0) scales[s][lane >> 3] = make_float4(ks, lv, inv, 0.f);
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&full[s]);
+                ++n;
+            }
+            block = next_block;
+            slot = next_slot;
         }
         ptx::cp_async_commit();
-        if (++stage_in == S::kStages) stage_in = 0;
-    };
-#pragma unroll
-    for (int s = 0; s < S::kStages - 1; ++s) fetch();
+        ptx::cp_async_wait<0>();                     // no copy is left on its way into memory that this CTA gives back
+        return;
+    }
 
-    int stage = 0;
+    uint32_t n = 0;                                  // steps so far
+    bool dead = false;                               // a wait gave up: what is left comes out NaN
+#pragma unroll 1
     for (int left = todo; left > 0;) {
         // ---- a tile of rows: its queries as fragments
         const int first = at.block, steps = min(left, at.blocks - at.block), rows = at.n * a.group;
-        __syncthreads();                             // the last tile's fragments and sums have been read
+        ar_sync();                                   // the last tile's fragments and sums have been read
         {
             constexpr int kPer = D / 8;              // elements of a thread: 8 threads a row
             const int r = tid >> 3, k = tid & 7, m = at.tile * kArRows + r;
@@ -251,7 +286,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
                 asm volatile("st.shared.b32 [%0], %1;" ::"r"(to), "r"(pack_half(f[e] * unit, f[e + 1] * unit)) : "memory");
             }
         }
-        __syncthreads();
+        ar_sync();
         // ends of this lane's two rows, of the tile's first and last one
         int end[2], lo_end, hi_end;
         {
@@ -266,110 +301,116 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
 #pragma unroll
         for (int j = 0; j < S::kNt; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
 
-        for (int b = 0; b < steps; ++b) {
-            ptx::cp_async_wait<S::kStages - 2>();
-            __syncwarp();                            // everyone's pieces are there; everyone is done with the stage before
-            fetch();
-            const int t0 = (first + b) * kArBlock + warp * 16;
-            const uint32_t kt = ring + stage * 2 * S::kTile, vt = kt + S::kTile;
-            const float2 sc = lds_f2(scales + stage * 8);
-            if (++stage == S::kStages) stage = 0;
-            if (t0 >= hi_end) continue;
-            // ---- scores of tokens t0 + 2c, 2c + 1 (s[0]) and 8 more (s[1]) for rows g, g + 8
-            float s[2][4] = {};
+        int t0 = first * kArBlock + warp * 16;
+        uint32_t stage = n % S::kStages, parity = n / S::kStages & 1;
+#pragma unroll 1
+        for (int b = 0; b < steps; ++b, t0 += kArBlock) {
+            if (!dead && !ptx::mbar_wait(&full[stage], parity)) dead = true;
+            const uint32_t kt = ring + stage * 2 * S::kBytes + warp * 16 * D, vt = kt + S::kBytes;
+            if (t0 < hi_end && !dead) {
+                const float4 sc = lds_f4(scales_u32 + (stage * kArWarps + warp) * 16);
+                // ---- scores of tokens t0 + 2c, 2c + 1 (s[0]) and 8 more (s[1]) for rows g, g + 8
+                float s[2][4] = {};
 #pragma unroll
-            for (int h = 0; h < D / 64; ++h) {
-                uint32_t w[2][4];
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const uint4 v = lds_v4(kt + ar_piece<D>(g + 8 * x, D == 128 ? 2 * c + h : c));
-                    w[x][0] = v.x ^ 0x80808080u;
-                    w[x][1] = v.y ^ 0x80808080u;
-                    w[x][2] = v.z ^ 0x80808080u;
-                    w[x][3] = v.w ^ 0x80808080u;
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint4 qf = lds_v4(frag + (uint32_t)(((h * 4 + e) * 32 + lane) * 16));
+                for (int h = 0; h < D / 64; ++h) {
+                    uint32_t w[2][4];
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        uint32_t b0, b1;
-                        codes_to_half(w[x][e], b0, b1);
-                        mma_f16(s[x], qf, b0, b1);
+                        const uint4 v = lds_v4(kt + ar_piece<D>(g + 8 * x, D == 128 ? 2 * c + h : c));
+                        w[x][0] = v.x ^ 0x80808080u;
+                        w[x][1] = v.y ^ 0x80808080u;
+                        w[x][2] = v.z ^ 0x80808080u;
+                        w[x][3] = v.w ^ 0x80808080u;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint4 qf = lds_v4(frag + (uint32_t)(((h * 4 + e) * 32 + lane) * 16));
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            uint32_t b0, b1;
+                            codes_to_half(w[x][e], b0, b1);
+                            mma_f16(s[x], qf, b0, b1);
+                        }
+                    }
+                }
+                // ---- weights
+                const float k0 = f0 * sc.x, k1 = f1 * sc.x;
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[x][e] = fmaf(s[x][e], e < 2 ? k0 : k1, sc.y);
+                const bool masked = t0 + 16 > lo_end;
+                if (masked) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (t0 + 8 * x + 2 * c + (e & 1) >= end[e >> 1]) s[x][e] = -INFINITY;
+                }
+                const float top0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
+                const float top1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
+                if (__any_sync(0xffffffffu, fmaxf(top0 - m[0], top1 - m[1]) > kAtSlack)) {
+                    float n0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, 1)), n1 = fmaxf(top1, __shfl_xor_sync(0xffffffffu, top1, 1));
+                    n0 = fmaxf(m[0], fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, 2)));
+                    n1 = fmaxf(m[1], fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, 2)));
+                    const float c0 = ex2(m[0] - n0), c1 = ex2(m[1] - n1);
+                    m[0] = n0;
+                    m[1] = n1;
+                    l[0] *= c0;
+                    l[1] *= c1;
+#pragma unroll
+                    for (int j = 0; j < S::kNt; ++j) {
+                        acc[j][0] *= c0;
+                        acc[j][1] *= c0;
+                        acc[j][2] *= c1;
+                        acc[j][3] *= c1;
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[x][e] = ex2(s[x][e] - m[e >> 1]);
+                {
+                    const float p0 = (s[0][0] + s[0][1]) + (s[1][0] + s[1][1]), p1 = (s[0][2] + s[0][3]) + (s[1][2] + s[1][3]);
+                    // weights of 0 add nothing, whatever the block's scale is (of one that the row does not see)
+                    if (!masked || p0 != 0.f) l[0] = fmaf(p0, sc.z, l[0]);
+                    if (!masked || p1 != 0.f) l[1] = fmaf(p1, sc.z, l[1]);
+                }
+                const uint4 pf = make_uint4(pack_half(s[0][0], s[0][1]), pack_half(s[0][2], s[0][3]), pack_half(s[1][0], s[1][1]),
+                                            pack_half(s[1][2], s[1][3]));
+                // ---- values: tokens 2c, 2c + 1, 2c + 8, 2c + 9, columns D / 8 * g ..
+                // (8 bytes at a time: 16 would be four more registers a token than there are)
+#pragma unroll
+                for (int half = 0; half < D / 64; ++half) {
+                    uint32_t v[4][2];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int t = 2 * c + (x & 1) + 8 * (x >> 1);
+                        const uint2 r = D == 128 ? lds_v2(vt + ar_piece<D>(t, g) + half * 8) : lds_v2(vt + ar_piece<D>(t, g >> 1) + (g & 1) * 8);
+                        v[x][0] = r.x ^ 0x80808080u;
+                        v[x][1] = r.y ^ 0x80808080u;
+                    }
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        uint32_t b0[4], b1[4];
+                        codes_to_half(__byte_perm(v[0][w], v[1][w], 0x5140), b0[0], b0[1]);
+                        codes_to_half(__byte_perm(v[0][w], v[1][w], 0x7362), b0[2], b0[3]);
+                        codes_to_half(__byte_perm(v[2][w], v[3][w], 0x5140), b1[0], b1[1]);
+                        codes_to_half(__byte_perm(v[2][w], v[3][w], 0x7362), b1[2], b1[3]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) mma_f16(acc[4 * (2 * half + w) + j], pf, b0[j], b1[j]);
                     }
                 }
             }
-            // ---- weights
-            float lv, inv;
-            value_scale(sc.y, lv, inv);
-            const float k0 = f0 * sc.x, k1 = f1 * sc.x;
-            const bool masked = t0 + 16 > lo_end;
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[x][e] = fmaf(s[x][e], e < 2 ? k0 : k1, lv);
-                    if (masked && t0 + 8 * x + 2 * c + (e & 1) >= end[e >> 1]) s[x][e] = -INFINITY;
-                }
-            }
-            const float top0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
-            const float top1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
-            if (__any_sync(0xffffffffu, top0 - m[0] > kAtSlack || top1 - m[1] > kAtSlack)) {
-                float n0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, 1)), n1 = fmaxf(top1, __shfl_xor_sync(0xffffffffu, top1, 1));
-                n0 = fmaxf(m[0], fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, 2)));
-                n1 = fmaxf(m[1], fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, 2)));
-                const float c0 = ex2(m[0] - n0), c1 = ex2(m[1] - n1);
-                m[0] = n0;
-                m[1] = n1;
-                l[0] *= c0;
-                l[1] *= c1;
-#pragma unroll
-                for (int j = 0; j < S::kNt; ++j) {
-                    acc[j][0] *= c0;
-                    acc[j][1] *= c0;
-                    acc[j][2] *= c1;
-                    acc[j][3] *= c1;
-                }
-            }
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = ex2(s[x][e] - m[e >> 1]);
-                    // a weight of 0 by the mask adds nothing, whatever its block's scale is
-                    if (!masked || s[x][e] != -INFINITY) l[e >> 1] = fmaf(p, inv, l[e >> 1]);
-                    s[x][e] = p;
-                }
-            const uint4 pf = make_uint4(pack_half(s[0][0], s[0][1]), pack_half(s[0][2], s[0][3]), pack_half(s[1][0], s[1][1]),
-                                        pack_half(s[1][2], s[1][3]));
-            // ---- values: tokens 2c, 2c + 1, 2c + 8, 2c + 9, columns D / 8 * g ..
-            uint32_t v[4][D / 32];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int t = 2 * c + (x & 1) + 8 * (x >> 1);
-                if (D == 128) {
-                    const uint4 r = lds_v4(vt + ar_piece<D>(t, g));
-                    v[x][0] = r.x ^ 0x80808080u;
-                    v[x][1] = r.y ^ 0x80808080u;
-                    v[x][D / 32 - 2] = r.z ^ 0x80808080u;
-                    v[x][D / 32 - 1] = r.w ^ 0x80808080u;
-                } else {
-                    const uint2 r = lds_v2(vt + ar_piece<D>(t, g >> 1) + (g & 1) * 8);
-                    v[x][0] = r.x ^ 0x80808080u;
-                    v[x][1] = r.y ^ 0x80808080u;
-                }
-            }
-#pragma unroll
-            for (int w = 0; w < D / 32; ++w) {
-                uint32_t b0[4], b1[4];
-                codes_to_half(__byte_perm(v[0][w], v[1][w], 0x5140), b0[0], b0[1]);
-                codes_to_half(__byte_perm(v[0][w], v[1][w], 0x7362), b0[2], b0[3]);
-                codes_to_half(__byte_perm(v[2][w], v[3][w], 0x5140), b1[0], b1[1]);
-                codes_to_half(__byte_perm(v[2][w], v[3][w], 0x7362), b1[2], b1[3]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) mma_f16(acc[4 * w + j], pf, b0[j], b1[j]);
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&empty[stage]);
+            if (++stage == S::kStages) {
+                stage = 0;
+                parity ^= 1u;
             }
         }
+        n += steps;
+        if (dead) l[0] = l[1] = __uint_as_float(0x7fc00000u);
 
         // ---- the warps' sums, put together in their order: to a common m', then 2 + 2, then 1 + 1
 #pragma unroll
@@ -378,7 +419,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
             l[x] += __shfl_xor_sync(0xffffffffu, l[x], 2);
             if (c == 0) row_ml[warp][g + 8 * x] = make_float2(m[x], l[x]);
         }
-        __syncthreads();
+        ar_sync();
         float sum_l[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -404,20 +445,21 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
             if (warp >= half && warp < 2 * half) {
 #pragma unroll
                 for (int j = 0; j < S::kNt; ++j)
-                    joined[((warp - half) * S::kNt + j) * 32 + lane] = make_float4(acc[j][0], acc[j][1], acc[j][2], acc[j][3]);
+                    ptx::st_shared_v4(joined + ((warp - half) * S::kNt + j) * 512,
+                                      make_uint4(__float_as_uint(acc[j][0]), __float_as_uint(acc[j][1]), __float_as_uint(acc[j][2]), __float_as_uint(acc[j][3])));
             }
-            __syncthreads();
+            ar_sync();
             if (warp < half) {
 #pragma unroll
                 for (int j = 0; j < S::kNt; ++j) {
-                    const float4 o = joined[(warp * S::kNt + j) * 32 + lane];
+                    const float4 o = ptx::ld_shared_v4(joined + (warp * S::kNt + j) * 512);
                     acc[j][0] += o.x;
                     acc[j][1] += o.y;
                     acc[j][2] += o.z;
                     acc[j][3] += o.w;
                 }
             }
-            if (half > 1) __syncthreads();
+            if (half > 1) ar_sync();
         }
         const bool whole = first == 0 && steps == at.blocks;
         if (warp == 0) {
@@ -467,9 +509,8 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
                                                    1 + (rest + chunk - 1) / chunk)
                                        : make_int4(0, 0, 0, 0);
         }
-        for (int b = 0; b < steps; ++b) at.next(a);
+        at.next(a, steps);
     }
-    ptx::cp_async_wait<0>();
 }
 
 // Puts the parts of tile (CTA blockIdx.x of the kernel above) together: a thread per row and four columns.

@@ -47,7 +47,8 @@ inline bool cache_view(const rtprune_cache_t *c, CacheView &v, rtprune_status_t 
     int shift = 4;
     while (shift < 7 && (1 << shift) != c->page_size) ++shift;
     if ((1 << shift) != c->page_size) return false;                              // 16, 32, 64, 128
-    if (c->num_pages > INT32_MAX / c->page_size || c->kv_heads > 1024) return false;   // slots are 32-bit
+    // slots are 32-bit, and so are the rows of codes
+    if (c->kv_heads > 1024 || c->num_pages > INT32_MAX / c->page_size / c->kv_heads) return false;
     if (c->head_dim != 64 && c->head_dim != 128) return false;
     v = {c->k, c->v, c->k_scale, c->v_scale, (int32_t)c->num_pages, c->kv_heads, c->head_dim, c->page_size, shift};
     status = RTPRUNE_OK;
