@@ -74,14 +74,16 @@ static bool queries_map(CUtensorMap *map, const AttendArgs &a, int heads, int to
     const cuuint32_t box[3] = {64, (cuuint32_t)heads, (cuuint32_t)tokens};
     return tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.q, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
-template <int D>
-static cudaError_t launch_rows(const AttendArgs &a, int ctas, uint8_t *ws, cudaStream_t st)
+template <int D, int R>
+static cudaError_t launch_rows(const AttendArgs &a, uint8_t *ws, cudaStream_t st)
 {
+    const int ctas = std::min(ArShape<D, R>::kPerSm * device_sms(), kArMostCtas);
+    if (!ctas) return cudaErrorInvalidDevice;
     const RowsLayout w = rows_layout(ctas, D);
     static std::atomic<unsigned long long> ready{0};             // devices that know the kernel's shared memory
-    cudaError_t e = allow_smem(attend_rows_kernel<D>, ArShape<D>::kSmem, ready);
+    cudaError_t e = allow_smem(attend_rows_kernel<D, R>, ArShape<D, R>::kSmem, ready);
     if (e != cudaSuccess) return e;
-    e = launch_chained(attend_rows_kernel<D>, dim3(ctas), dim3(kArThreads), (size_t)ArShape<D>::kSmem, st, a, (float *)(ws + w.part),
+    e = launch_chained(attend_rows_kernel<D, R>, dim3(ctas), dim3(kArThreads), (size_t)ArShape<D, R>::kSmem, st, a, (float *)(ws + w.part),
                        (float2 *)(ws + w.part_ml), (int4 *)(ws + w.join));
     if (e != cudaSuccess) return e;
     return launch_chained(attend_join_kernel<D>, dim3(ctas), dim3(kArRows * D / 4), (size_t)0, st, a, (const float *)(ws + w.part),
@@ -151,11 +153,11 @@ extern "C" rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *
                     q_heads / c.kv_heads, max_q_len, (int)max_seq_len, max_pages, c, scale * 1.4426950408889634f, causal ? 1 : 0,
                     (__nv_bfloat16 *)out, lse};
     if (few_rows(max_q_len, a.group)) {
-        const int ctas = std::min(kArPerSm * device_sms(), kArMostCtas);
-        if (!ctas) return RTPRUNE_ERR_CUDA;
         uint8_t *ws = (uint8_t *)workspace;
-        const cudaError_t e = c.dim == 128 ? launch_rows<128>(a, ctas, ws, (cudaStream_t)cuda_stream)
-                                           : launch_rows<64>(a, ctas, ws, (cudaStream_t)cuda_stream);
+        cudaStream_t st = (cudaStream_t)cuda_stream;
+        const bool eight = (int64_t)max_q_len * a.group <= 8;
+        const cudaError_t e = c.dim == 128 ? eight ? launch_rows<128, 8>(a, ws, st) : launch_rows<128, 16>(a, ws, st)
+                                           : eight ? launch_rows<64, 8>(a, ws, st) : launch_rows<64, 16>(a, ws, st);
         if (e != cudaSuccess) return RTPRUNE_ERR_CUDA;
         return cudaGetLastError() == cudaSuccess ? RTPRUNE_OK : RTPRUNE_ERR_CUDA;
     }

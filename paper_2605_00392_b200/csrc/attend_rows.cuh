@@ -1,11 +1,13 @@
 // Attention of few query rows per kv head (single tokens, a few drafted ones) over the 8-bit paged cache: bound by reading
 // the codes once.
 //
-// A tile of 16 rows (a token's heads of one kv head, token by token) against 64 tokens a step, a warp 16 of them, on
-// mma.sync m16n8k16: at one or a few rows the tensor cores are idle either way (a step of 8 KB and 16 rows has 0.3 us of HBM
-// time per SM and 0.02 of mma), and its fragments come straight out of 16-byte loads because both contractions may run in any order:
+// A tile of rows (a token's heads of one kv head, token by token) against 64 tokens a step, a warp 16 of them, on mma.sync m16n8k16: at one
+// or a few rows the tensor cores are idle either way (a step of 16 KB has 0.7 us of HBM time per SM and 0.02 of mma), and its fragments come
+// straight out of 16-byte pieces because both contractions may run in any order:
 //   scores  a lane takes 32 (D = 64: 16) neighbouring elements of a token's key; the queries' fragments are laid out to match
-//   values  a lane takes 16 (8) neighbouring columns of four tokens: n-tile j of the output is column 16 g + j of each lane group g
+//   values  a lane takes 16 (8) neighbouring columns of four tokens
+// Tiles of 16 rows have the rows as the mma's 16 and tokens or columns as its 8.  Calls of at most 8 rows a kv head have tiles of 8, the other way round:
+// half the mma, half the accumulators, half the softmax; the weights change sides by movmatrix.
 // Codes come by 16-byte cp.async into a ring of steps in shared memory, the pieces swizzled by row so that both ways of reading find them in
 // different banks; a fifth warp fetches them, with the scales of their blocks, and walks the tables: the four others have nothing but
 // the arithmetic, about 300 instructions for 16 tokens, and that is what HBM is kept waiting by (with the fetching in the same warps it
@@ -23,18 +25,19 @@ namespace rtp {
 constexpr int kArWarps = 4;                          // that compute; one more fetches
 constexpr int kArThreads = 32 * (kArWarps + 1);
 constexpr int kArBlock = 16 * kArWarps;              // tokens of a step
-constexpr int kArPerSm = 2;                          // CTAs of an SM (three leave a thread 128 registers, which spill)
-constexpr int kArMostCtas = kArPerSm * 160;          // what the workspace is sized for (a B200 has 148 SMs)
+constexpr int kArMostCtas = 3 * 160;                 // what the workspace is sized for (a B200 has 148 SMs)
 constexpr int kArRows = 16;
 constexpr int kArLeast = 4;                          // blocks of a run at least
 
-template <int D> struct ArShape {
-    static constexpr int kStages = D == 128 ? 5 : 10;
+template <int D, int R> struct ArShape {
+    // CTAs of an SM (with 16 rows three would leave a thread 128 registers, which spill: no kernel here may have a stack frame)
+    static constexpr int kPerSm = R == 8 ? 3 : 2;
+    static constexpr int kStages = (R == 8 ? 4 : 5) * (D == 128 ? 1 : 2);
     static constexpr int kBytes = kArBlock * D;      // keys (or values) of a step
     static constexpr int kSteps = D / 16;            // mma steps of a score
-    static constexpr int kNt = D / 8;                // n-tiles of the output
+    static constexpr int kNt = R == 8 ? D / 16 : D / 8;            // mma tiles of the output
     static constexpr int kRing = kStages * 2 * kBytes;
-    static constexpr int kFrag = kSteps * 32 * 16;   // the queries' fragments
+    static constexpr int kFrag = R == 8 ? 0 : kSteps * 32 * 16;    // the queries' fragments
     static constexpr int kJoin = (kArWarps / 2) * 32 * kNt * 16;   // accumulators of half the warps
     static constexpr int kSmem = kRing + kFrag + kJoin + 1024 /*alignment*/;
 };
@@ -44,18 +47,18 @@ struct ArPlace {
     int i, head, tile, block;                        // request, kv head, tile of rows, block of tokens
     int row0, n, len, blocks, tiles;                 // of the request
 
-    __device__ void request(const AttendArgs &a, int at)
+    template <int R> __device__ void request(const AttendArgs &a, int at)
     {
         i = at;
         head = tile = block = 0;
         tiles = 0;
         if (i < a.batch && attend_request(a, i, row0, n, len)) {
-            tiles = (n * a.group + kArRows - 1) / kArRows;
+            tiles = (n * a.group + R - 1) / R;
             blocks = max(1, (len + kArBlock - 1) / kArBlock);
         }
     }
     // `steps` blocks on, within the tile or to the next one's first (the line ends before the batch does: the caller counts)
-    __device__ void next(const AttendArgs &a, int steps)
+    template <int R> __device__ void next(const AttendArgs &a, int steps)
     {
         block += steps;
         if (block < blocks) return;
@@ -63,27 +66,27 @@ struct ArPlace {
         if (++tile < tiles) return;
         tile = 0;
         if (++head < a.c.kv_heads) return;
-        do request(a, i + 1);
+        do request<R>(a, i + 1);
         while (tiles == 0 && i < a.batch);
     }
 };
 
-__device__ inline int64_t ar_units(const AttendArgs &a, int i)
+template <int R> __device__ inline int64_t ar_units(const AttendArgs &a, int i)
 {
     int row0, n, len;
     if (!attend_request(a, i, row0, n, len)) return 0;
-    return (int64_t)((n * a.group + kArRows - 1) / kArRows) * a.c.kv_heads * max(1, (len + kArBlock - 1) / kArBlock);
+    return (int64_t)((n * a.group + R - 1) / R) * a.c.kv_heads * max(1, (len + kArBlock - 1) / kArBlock);
 }
 
 // Where CTA `blockIdx.x` of the line begins, and how many blocks it takes (0: none).
-__device__ inline int ar_find(const AttendArgs &a, ArPlace &at, int &chunk)
+template <int R> __device__ inline int ar_find(const AttendArgs &a, ArPlace &at, int &chunk)
 {
     __shared__ int64_t warp_units[kArWarps + 1], found_before;
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (a.batch + kArThreads - 1) / kArThreads, i0 = min(tid * per, a.batch), i1 = min(i0 + per, a.batch);
     int64_t mine = 0;
-    for (int i = i0; i < i1; ++i) mine += ar_units(a, i);
+    for (int i = i0; i < i1; ++i) mine += ar_units<R>(a, i);
     int64_t upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -104,12 +107,12 @@ __device__ inline int ar_find(const AttendArgs &a, ArPlace &at, int &chunk)
     if (start >= total) return 0;
     if (start >= before && start < before + mine) {
         int i = i0;
-        for (int64_t u; (u = ar_units(a, i)) <= start - before; ++i) before += u;
+        for (int64_t u; (u = ar_units<R>(a, i)) <= start - before; ++i) before += u;
         found = i;
         found_before = before;
     }
     __syncthreads();
-    at.request(a, found);
+    at.request<R>(a, found);
     const int64_t rel = start - found_before;
     at.block = (int)(rel % at.blocks);
     at.tile = (int)(rel / at.blocks % at.tiles);
@@ -158,18 +161,26 @@ template <int D> __device__ inline uint32_t ar_piece(int t, int ch)
     return (uint32_t)(line * 128 + ((((t & 1) * 4 + ch) ^ ((line & 3) << 1)) << 4));
 }
 
+// An 8 x 8 matrix of fp16, a row's two neighbouring elements a lane, to its transpose.
+__device__ inline uint32_t mat_trans(uint32_t x)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+
 // Parts of a tile that a cut goes through: `part` [2 per CTA][16][D] sums, `part_ml` [2 per CTA][16] (m', l).  A part that holds its
 // tile's first block is the CTA's second, any other its first.  join[CTA]: the tile that begins in the CTA and does not end in it:
 // (first row of the request, kv head, the tile's first row | its rows << 26, CTAs that it goes through; 0: there is none).
-template <int D>
-__global__ void __launch_bounds__(kArThreads, kArPerSm)
+template <int D, int R>
+__global__ void __launch_bounds__(kArThreads, ArShape<D, R>::kPerSm)
 attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ part, float2 *__restrict__ part_ml, int4 *__restrict__ join)
 {
-    using S = ArShape<D>;
+    using S = ArShape<D, R>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ float row_factor[kArRows];
-    __shared__ float2 row_ml[kArWarps][kArRows];
+    __shared__ float2 row_ml[kArWarps][R];
     __shared__ float4 scales[S::kStages][kArWarps];  // ks, log2 vs, 1 / vs of each warp's 16 tokens
     __shared__ uint64_t full[S::kStages], empty[S::kStages];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
@@ -186,7 +197,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
     ptx::grid_dep_wait();
     ArPlace at;
     int chunk;
-    const int todo = ar_find(a, at, chunk);          // (its barriers order the initialisation too)
+    const int todo = ar_find<R>(a, at, chunk);          // (its barriers order the initialisation too)
     if (todo == 0) {
         if (tid == 0) join[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
@@ -206,7 +217,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
                 const int page = t < at.len ? attend_page(a, at.i, t) : -1;
                 next_block = page < 0 ? -1 : page * a.c.kv_heads + at.head;
                 next_slot = t & (a.c.page_size - 1);
-                at.next(a, 1);
+                at.next<R>(a, 1);
             }
             if (look > 0) {
                 const uint32_t s = n % S::kStages, turn = n / S::kStages, to = ring + s * 2 * S::kBytes;
@@ -249,54 +260,92 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
     for (int left = todo; left > 0;) {
         // ---- a tile of rows: its queries as fragments
         const int first = at.block, steps = min(left, at.blocks - at.block), rows = at.n * a.group;
-        ar_sync();                                   // the last tile's fragments and sums have been read
-        {
-            constexpr int kPer = D / 8;              // elements of a thread: 8 threads a row
-            const int r = tid >> 3, k = tid & 7, m = at.tile * kArRows + r;
-            uint4 raw[kPer / 8];
+        float f0, f1;                                // factors of this lane's two rows
+        uint32_t qf[R == 8 ? S::kSteps * 2 : 1];     // 8 rows: this lane's fragments
+        if constexpr (R == 8) {
+            // row g, elements D / 4 * c ..
+            const int m = at.tile * R + g, j = min(m, rows - 1) / a.group, h = at.head * a.group + (min(m, rows - 1) - j * a.group);
+            const uint4 *p = reinterpret_cast<const uint4 *>(a.q + (int64_t)(at.row0 + j) * a.q_stride + (int64_t)h * D + c * (D / 4));
+            uint4 raw[D / 32];
 #pragma unroll
-            for (int e = 0; e < kPer / 8; ++e) raw[e] = make_uint4(0u, 0u, 0u, 0u);
-            if (m < rows) {
-                const int j = m / a.group, h = at.head * a.group + (m - j * a.group);
-                const uint4 *p = reinterpret_cast<const uint4 *>(a.q + (int64_t)(at.row0 + j) * a.q_stride + (int64_t)h * D + k * kPer);
-#pragma unroll
-                for (int e = 0; e < kPer / 8; ++e) raw[e] = __ldg(p + e);
+            for (int e = 0; e < D / 32; ++e) {
+                raw[e] = make_uint4(0u, 0u, 0u, 0u);
+                if (m < rows) raw[e] = __ldg(p + e);
             }
-            float f[kPer], top = 0.f;
+            float top = 0.f;
 #pragma unroll
-            for (int e = 0; e < kPer / 8; ++e) {
+            for (int e = 0; e < D / 32; ++e) {
                 float t8[8];
                 Elem<__nv_bfloat16>::unpack(raw[e], t8);
 #pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    f[8 * e + x] = t8[x];
-                    top = max_nan(top, fabsf(t8[x]));
-                }
+                for (int x = 0; x < 8; ++x) top = max_nan(top, fabsf(t8[x]));
             }
-#pragma unroll
-            for (int o = 1; o < 8; o <<= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+            top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 2));
             float factor;
             const float unit = query_scale(top, a.scale_log2, factor);
-            if (k == 0) row_factor[r] = factor;
-            // element d: lane (r & 7) * 4 + d / (D / 4), step (d mod D / 4) / 4, register (d & 2) + (r >= 8)
 #pragma unroll
-            for (int e = 0; e < kPer; e += 2) {
-                const int d = k * kPer + e, lane_to = (r & 7) * 4 + d / (D / 4), step = d % (D / 4) / 4;
-                const uint32_t to = frag + (uint32_t)((step * 32 + lane_to) * 16 + ((d & 2) + (r >> 3)) * 4);
-                asm volatile("st.shared.b32 [%0], %1;" ::"r"(to), "r"(pack_half(f[e] * unit, f[e + 1] * unit)) : "memory");
+            for (int e = 0; e < D / 32; ++e) {
+                float t8[8];
+                Elem<__nv_bfloat16>::unpack(raw[e], t8);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) qf[4 * e + x] = pack_half(t8[2 * x] * unit, t8[2 * x + 1] * unit);
             }
+            f0 = __shfl_sync(0xffffffffu, factor, 8 * c);
+            f1 = __shfl_sync(0xffffffffu, factor, 8 * c + 4);
+        } else {
+            ar_sync();                                   // the last tile's fragments and sums have been read
+            {
+                constexpr int kPer = D / 8;              // elements of a thread: 8 threads a row
+                const int r = tid >> 3, k = tid & 7, m = at.tile * R + r;
+                uint4 raw[kPer / 8];
+#pragma unroll
+                for (int e = 0; e < kPer / 8; ++e) raw[e] = make_uint4(0u, 0u, 0u, 0u);
+                if (m < rows) {
+                    const int j = m / a.group, h = at.head * a.group + (m - j * a.group);
+                    const uint4 *p = reinterpret_cast<const uint4 *>(a.q + (int64_t)(at.row0 + j) * a.q_stride + (int64_t)h * D + k * kPer);
+#pragma unroll
+                    for (int e = 0; e < kPer / 8; ++e) raw[e] = __ldg(p + e);
+                }
+                float f[kPer], top = 0.f;
+#pragma unroll
+                for (int e = 0; e < kPer / 8; ++e) {
+                    float t8[8];
+                    Elem<__nv_bfloat16>::unpack(raw[e], t8);
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) {
+                        f[8 * e + x] = t8[x];
+                        top = max_nan(top, fabsf(t8[x]));
+                    }
+                }
+#pragma unroll
+                for (int o = 1; o < 8; o <<= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+                float factor;
+                const float unit = query_scale(top, a.scale_log2, factor);
+                if (k == 0) row_factor[r] = factor;
+                // element d: lane (r & 7) * 4 + d / (D / 4), step (d mod D / 4) / 4, register (d & 2) + (r >= 8)
+#pragma unroll
+                for (int e = 0; e < kPer; e += 2) {
+                    const int d = k * kPer + e, lane_to = (r & 7) * 4 + d / (D / 4), step = d % (D / 4) / 4;
+                    const uint32_t to = frag + (uint32_t)((step * 32 + lane_to) * 16 + ((d & 2) + (r >> 3)) * 4);
+                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(to), "r"(pack_half(f[e] * unit, f[e + 1] * unit)) : "memory");
+                }
+            }
+            ar_sync();
+            f0 = row_factor[g];
+            f1 = row_factor[g + 8];
         }
-        ar_sync();
+        // this lane's two rows: 2c, 2c + 1 of 8, or g, g + 8 of 16
+        const int mine[2] = {R == 8 ? 2 * c : g, R == 8 ? 2 * c + 1 : g + 8};
         // ends of this lane's two rows, of the tile's first and last one
         int end[2], lo_end, hi_end;
         {
-            const int m0 = at.tile * kArRows, last = min(m0 + kArRows, rows) - 1, len = max(at.len, 0), past = len - at.n + 1;
-            end[0] = a.causal ? min(len, past + min(m0 + g, last) / a.group) : len;
-            end[1] = a.causal ? min(len, past + min(m0 + g + 8, last) / a.group) : len;
+            const int m0 = at.tile * R, last = min(m0 + R, rows) - 1, len = max(at.len, 0), past = len - at.n + 1;
+            end[0] = a.causal ? min(len, past + min(m0 + mine[0], last) / a.group) : len;
+            end[1] = a.causal ? min(len, past + min(m0 + mine[1], last) / a.group) : len;
             lo_end = a.causal ? min(len, past + m0 / a.group) : len;
             hi_end = a.causal ? min(len, past + last / a.group) : len;
         }
-        const float f0 = row_factor[g], f1 = row_factor[g + 8];
         float acc[S::kNt][4], m[2] = {kAtNothing, kAtNothing}, l[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < S::kNt; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
@@ -309,96 +358,177 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
             const uint32_t kt = ring + stage * 2 * S::kBytes + warp * 16 * D, vt = kt + S::kBytes;
             if (t0 < hi_end && !dead) {
                 const float4 sc = lds_f4(scales_u32 + (stage * kArWarps + warp) * 16);
-                // ---- scores of tokens t0 + 2c, 2c + 1 (s[0]) and 8 more (s[1]) for rows g, g + 8
-                float s[2][4] = {};
+                if constexpr (R == 8) {
+                    // ---- scores of tokens t0 + g (s[0], s[1]) and 8 more (s[2], s[3]) for rows 2c, 2c + 1
+                    float s[4] = {};
 #pragma unroll
-                for (int h = 0; h < D / 64; ++h) {
-                    uint32_t w[2][4];
+                    for (int h = 0; h < D / 64; ++h) {
+                        const uint4 k0 = lds_v4(kt + ar_piece<D>(g, D == 128 ? 2 * c + h : c)), k1 = lds_v4(kt + ar_piece<D>(g + 8, D == 128 ? 2 * c + h : c));
+                        const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const uint4 v = lds_v4(kt + ar_piece<D>(g + 8 * x, D == 128 ? 2 * c + h : c));
-                        w[x][0] = v.x ^ 0x80808080u;
-                        w[x][1] = v.y ^ 0x80808080u;
-                        w[x][2] = v.z ^ 0x80808080u;
-                        w[x][3] = v.w ^ 0x80808080u;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint4 qf = lds_v4(frag + (uint32_t)(((h * 4 + e) * 32 + lane) * 16));
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            uint32_t b0, b1;
-                            codes_to_half(w[x][e], b0, b1);
-                            mma_f16(s[x], qf, b0, b1);
+                        for (int e = 0; e < 4; ++e) {
+                            uint4 ka;
+                            codes_to_half(w0[e] ^ 0x80808080u, ka.x, ka.z);
+                            codes_to_half(w1[e] ^ 0x80808080u, ka.y, ka.w);
+                            mma_f16(s, ka, qf[2 * (h * 4 + e)], qf[2 * (h * 4 + e) + 1]);
                         }
                     }
-                }
-                // ---- weights
-                const float k0 = f0 * sc.x, k1 = f1 * sc.x;
+                    // ---- weights
+                    const float k0 = f0 * sc.x, k1 = f1 * sc.x;
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
+                    for (int e = 0; e < 4; ++e) s[e] = fmaf(s[e], e & 1 ? k1 : k0, sc.y);
+                    const bool masked = t0 + 16 > lo_end;
+                    if (masked) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[x][e] = fmaf(s[x][e], e < 2 ? k0 : k1, sc.y);
-                const bool masked = t0 + 16 > lo_end;
-                if (masked) {
+                        for (int e = 0; e < 4; ++e)
+                            if (t0 + g + 8 * (e >> 1) >= end[e & 1]) s[e] = -INFINITY;
+                    }
+                    const float top0 = fmaxf(s[0], s[2]), top1 = fmaxf(s[1], s[3]);
+                    if (__any_sync(0xffffffffu, fmaxf(top0 - m[0], top1 - m[1]) > kAtSlack)) {
+                        float n0 = top0, n1 = top1;
+#pragma unroll
+                        for (int o = 4; o < 32; o <<= 1) {
+                            n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, o));
+                            n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, o));
+                        }
+                        n0 = fmaxf(m[0], n0);
+                        n1 = fmaxf(m[1], n1);
+                        const float c0 = ex2(m[0] - n0), c1 = ex2(m[1] - n1);
+                        m[0] = n0;
+                        m[1] = n1;
+                        l[0] *= c0;
+                        l[1] *= c1;
+#pragma unroll
+                        for (int j = 0; j < S::kNt; ++j) {
+                            acc[j][0] *= c0;
+                            acc[j][1] *= c1;
+                            acc[j][2] *= c0;
+                            acc[j][3] *= c1;
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[e] = ex2(s[e] - m[e & 1]);
+                    {
+                        const float p0 = s[0] + s[2], p1 = s[1] + s[3];
+                        // weights of 0 add nothing, whatever the block's scale is (of one that the row does not see)
+                        if (!masked || p0 != 0.f) l[0] = fmaf(p0, sc.z, l[0]);
+                        if (!masked || p1 != 0.f) l[1] = fmaf(p1, sc.z, l[1]);
+                    }
+                    const uint32_t b0 = mat_trans(pack_half(s[0], s[1])), b1 = mat_trans(pack_half(s[2], s[3]));
+                    // ---- values: tokens 2c, 2c + 1, 2c + 8, 2c + 9, columns D / 8 * g ..: mma tile j has columns 2j and 2j + 1 of these
+#pragma unroll
+                    for (int half = 0; half < D / 64; ++half) {
+                        uint32_t v[4][2];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const int t = 2 * c + (x & 1) + 8 * (x >> 1);
+                            const uint2 r = D == 128 ? lds_v2(vt + ar_piece<D>(t, g) + half * 8) : lds_v2(vt + ar_piece<D>(t, g >> 1) + (g & 1) * 8);
+                            v[x][0] = r.x ^ 0x80808080u;
+                            v[x][1] = r.y ^ 0x80808080u;
+                        }
+#pragma unroll
+                        for (int w = 0; w < 2; ++w) {
+                            uint4 va, vb;
+                            codes_to_half(__byte_perm(v[0][w], v[1][w], 0x5140), va.x, va.y);
+                            codes_to_half(__byte_perm(v[2][w], v[3][w], 0x5140), va.z, va.w);
+                            codes_to_half(__byte_perm(v[0][w], v[1][w], 0x7362), vb.x, vb.y);
+                            codes_to_half(__byte_perm(v[2][w], v[3][w], 0x7362), vb.z, vb.w);
+                            mma_f16(acc[2 * (2 * half + w)], va, b0, b1);
+                            mma_f16(acc[2 * (2 * half + w) + 1], vb, b0, b1);
+                        }
+                    }
+                } else {
+                    // ---- scores of tokens t0 + 2c, 2c + 1 (s[0]) and 8 more (s[1]) for rows g, g + 8
+                    float s[2][4] = {};
+#pragma unroll
+                    for (int h = 0; h < D / 64; ++h) {
+                        uint32_t w[2][4];
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const uint4 v = lds_v4(kt + ar_piece<D>(g + 8 * x, D == 128 ? 2 * c + h : c));
+                            w[x][0] = v.x ^ 0x80808080u;
+                            w[x][1] = v.y ^ 0x80808080u;
+                            w[x][2] = v.z ^ 0x80808080u;
+                            w[x][3] = v.w ^ 0x80808080u;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint4 qf = lds_v4(frag + (uint32_t)(((h * 4 + e) * 32 + lane) * 16));
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                uint32_t b0, b1;
+                                codes_to_half(w[x][e], b0, b1);
+                                mma_f16(s[x], qf, b0, b1);
+                            }
+                        }
+                    }
+                    // ---- weights
+                    const float k0 = f0 * sc.x, k1 = f1 * sc.x;
 #pragma unroll
                     for (int x = 0; x < 2; ++x)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (t0 + 8 * x + 2 * c + (e & 1) >= end[e >> 1]) s[x][e] = -INFINITY;
-                }
-                const float top0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
-                const float top1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
-                if (__any_sync(0xffffffffu, fmaxf(top0 - m[0], top1 - m[1]) > kAtSlack)) {
-                    float n0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, 1)), n1 = fmaxf(top1, __shfl_xor_sync(0xffffffffu, top1, 1));
-                    n0 = fmaxf(m[0], fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, 2)));
-                    n1 = fmaxf(m[1], fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, 2)));
-                    const float c0 = ex2(m[0] - n0), c1 = ex2(m[1] - n1);
-                    m[0] = n0;
-                    m[1] = n1;
-                    l[0] *= c0;
-                    l[1] *= c1;
+                        for (int e = 0; e < 4; ++e) s[x][e] = fmaf(s[x][e], e < 2 ? k0 : k1, sc.y);
+                    const bool masked = t0 + 16 > lo_end;
+                    if (masked) {
 #pragma unroll
-                    for (int j = 0; j < S::kNt; ++j) {
-                        acc[j][0] *= c0;
-                        acc[j][1] *= c0;
-                        acc[j][2] *= c1;
-                        acc[j][3] *= c1;
+                        for (int x = 0; x < 2; ++x)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (t0 + 8 * x + 2 * c + (e & 1) >= end[e >> 1]) s[x][e] = -INFINITY;
                     }
-                }
+                    const float top0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
+                    const float top1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
+                    if (__any_sync(0xffffffffu, fmaxf(top0 - m[0], top1 - m[1]) > kAtSlack)) {
+                        float n0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, 1)), n1 = fmaxf(top1, __shfl_xor_sync(0xffffffffu, top1, 1));
+                        n0 = fmaxf(m[0], fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, 2)));
+                        n1 = fmaxf(m[1], fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, 2)));
+                        const float c0 = ex2(m[0] - n0), c1 = ex2(m[1] - n1);
+                        m[0] = n0;
+                        m[1] = n1;
+                        l[0] *= c0;
+                        l[1] *= c1;
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[x][e] = ex2(s[x][e] - m[e >> 1]);
-                {
-                    const float p0 = (s[0][0] + s[0][1]) + (s[1][0] + s[1][1]), p1 = (s[0][2] + s[0][3]) + (s[1][2] + s[1][3]);
-                    // weights of 0 add nothing, whatever the block's scale is (of one that the row does not see)
-                    if (!masked || p0 != 0.f) l[0] = fmaf(p0, sc.z, l[0]);
-                    if (!masked || p1 != 0.f) l[1] = fmaf(p1, sc.z, l[1]);
-                }
-                const uint4 pf = make_uint4(pack_half(s[0][0], s[0][1]), pack_half(s[0][2], s[0][3]), pack_half(s[1][0], s[1][1]),
-                                            pack_half(s[1][2], s[1][3]));
-                // ---- values: tokens 2c, 2c + 1, 2c + 8, 2c + 9, columns D / 8 * g ..
-                // (8 bytes at a time: 16 would be four more registers a token than there are)
-#pragma unroll
-                for (int half = 0; half < D / 64; ++half) {
-                    uint32_t v[4][2];
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int t = 2 * c + (x & 1) + 8 * (x >> 1);
-                        const uint2 r = D == 128 ? lds_v2(vt + ar_piece<D>(t, g) + half * 8) : lds_v2(vt + ar_piece<D>(t, g >> 1) + (g & 1) * 8);
-                        v[x][0] = r.x ^ 0x80808080u;
-                        v[x][1] = r.y ^ 0x80808080u;
+                        for (int j = 0; j < S::kNt; ++j) {
+                            acc[j][0] *= c0;
+                            acc[j][1] *= c0;
+                            acc[j][2] *= c1;
+                            acc[j][3] *= c1;
+                        }
                     }
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        uint32_t b0[4], b1[4];
-                        codes_to_half(__byte_perm(v[0][w], v[1][w], 0x5140), b0[0], b0[1]);
-                        codes_to_half(__byte_perm(v[0][w], v[1][w], 0x7362), b0[2], b0[3]);
-                        codes_to_half(__byte_perm(v[2][w], v[3][w], 0x5140), b1[0], b1[1]);
-                        codes_to_half(__byte_perm(v[2][w], v[3][w], 0x7362), b1[2], b1[3]);
+                    for (int x = 0; x < 2; ++x)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) mma_f16(acc[4 * (2 * half + w) + j], pf, b0[j], b1[j]);
+                        for (int e = 0; e < 4; ++e) s[x][e] = ex2(s[x][e] - m[e >> 1]);
+                    {
+                        const float p0 = (s[0][0] + s[0][1]) + (s[1][0] + s[1][1]), p1 = (s[0][2] + s[0][3]) + (s[1][2] + s[1][3]);
+                        // weights of 0 add nothing, whatever the block's scale is (of one that the row does not see)
+                        if (!masked || p0 != 0.f) l[0] = fmaf(p0, sc.z, l[0]);
+                        if (!masked || p1 != 0.f) l[1] = fmaf(p1, sc.z, l[1]);
+                    }
+                    const uint4 pf = make_uint4(pack_half(s[0][0], s[0][1]), pack_half(s[0][2], s[0][3]), pack_half(s[1][0], s[1][1]),
+                                                pack_half(s[1][2], s[1][3]));
+                    // ---- values: tokens 2c, 2c + 1, 2c + 8, 2c + 9, columns D / 8 * g ..
+                    // (8 bytes at a time: 16 would be four more registers a token than there are)
+#pragma unroll
+                    for (int half = 0; half < D / 64; ++half) {
+                        uint32_t v[4][2];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const int t = 2 * c + (x & 1) + 8 * (x >> 1);
+                            const uint2 r = D == 128 ? lds_v2(vt + ar_piece<D>(t, g) + half * 8) : lds_v2(vt + ar_piece<D>(t, g >> 1) + (g & 1) * 8);
+                            v[x][0] = r.x ^ 0x80808080u;
+                            v[x][1] = r.y ^ 0x80808080u;
+                        }
+#pragma unroll
+                        for (int w = 0; w < 2; ++w) {
+                            uint32_t b0[4], b1[4];
+                            codes_to_half(__byte_perm(v[0][w], v[1][w], 0x5140), b0[0], b0[1]);
+                            codes_to_half(__byte_perm(v[0][w], v[1][w], 0x7362), b0[2], b0[3]);
+                            codes_to_half(__byte_perm(v[2][w], v[3][w], 0x5140), b1[0], b1[1]);
+                            codes_to_half(__byte_perm(v[2][w], v[3][w], 0x7362), b1[2], b1[3]);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) mma_f16(acc[4 * (2 * half + w) + j], pf, b0[j], b1[j]);
+                        }
                     }
                 }
             }
@@ -415,9 +545,10 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
         // ---- the warps' sums, put together in their order: to a common m', then 2 + 2, then 1 + 1
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            l[x] += __shfl_xor_sync(0xffffffffu, l[x], 1);
-            l[x] += __shfl_xor_sync(0xffffffffu, l[x], 2);
-            if (c == 0) row_ml[warp][g + 8 * x] = make_float2(m[x], l[x]);
+            // over the lanes of a row: the four of a g, or the eight of a c
+#pragma unroll
+            for (int o = R == 8 ? 4 : 1; o < (R == 8 ? 32 : 4); o <<= 1) l[x] += __shfl_xor_sync(0xffffffffu, l[x], o);
+            if (R == 8 ? g == 0 : c == 0) row_ml[warp][mine[x]] = make_float2(m[x], l[x]);
         }
         ar_sync();
         float sum_l[2];
@@ -425,19 +556,19 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
         for (int x = 0; x < 2; ++x) {
             float top = kAtNothing;
 #pragma unroll
-            for (int w = 0; w < kArWarps; ++w) top = fmaxf(top, row_ml[w][g + 8 * x].x);
+            for (int w = 0; w < kArWarps; ++w) top = fmaxf(top, row_ml[w][mine[x]].x);
             sum_l[x] = 0.f;
 #pragma unroll
             for (int w = 0; w < kArWarps; ++w) {
-                const float2 ml = row_ml[w][g + 8 * x];
+                const float2 ml = row_ml[w][mine[x]];
                 sum_l[x] += ml.y * ex2(ml.x - top);
             }
             const float k = ex2(m[x] - top);
             m[x] = top;
 #pragma unroll
             for (int j = 0; j < S::kNt; ++j) {
-                acc[j][2 * x] *= k;
-                acc[j][2 * x + 1] *= k;
+                acc[j][R == 8 ? x : 2 * x] *= k;
+                acc[j][R == 8 ? x + 2 : 2 * x + 1] *= k;
             }
         }
 #pragma unroll
@@ -463,40 +594,40 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
         }
         const bool whole = first == 0 && steps == at.blocks;
         if (warp == 0) {
-            // lane (g, c) has columns D / 4 * c .. of rows g, g + 8: column n-tile j, c0 / c1 = j / j + D / 8
+            // 16 rows: lane (g, c) has columns D / 4 * c .. of rows g, g + 8: column n-tile j, c0 / c1 = j / j + D / 8
+            // 8 rows: columns D / 8 * g .. of rows 2c, 2c + 1: column 2j (+ 1) in c0, c1 (c2, c3) of tile j
+            constexpr int kCols = R == 8 ? D / 8 : D / 4;
+            auto value = [&](int x, int e) {
+                if constexpr (R == 8) return acc[e / 2][2 * (e & 1) + x];
+                else return acc[e % (D / 8)][2 * x + e / (D / 8)];
+            };
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                const int r = g + 8 * x, mr = at.tile * kArRows + r;
+                const int r = mine[x], mr = at.tile * R + r, col = (R == 8 ? g : c) * kCols;
                 if (mr >= rows) continue;
-                const int slot = 2 * blockIdx.x + (first == 0 ? 1 : 0);
+                const bool lead = R == 8 ? g == 0 : c == 0;
                 if (whole) {
                     const bool nan = at.len < 0;
                     const float k = nan ? __uint_as_float(0x7fc00000u) : sum_l[x] == 0.f ? 0.f : 1.f / sum_l[x];
                     const int j = mr / a.group;
                     const int64_t o = (int64_t)(at.row0 + j) * a.q_heads + at.head * a.group + (mr - j * a.group);
-                    __nv_bfloat16 *to = a.out + o * D + c * (D / 4);
+                    __nv_bfloat16 *to = a.out + o * D + col;
 #pragma unroll
-                    for (int y = 0; y < 2; ++y)
+                    for (int e = 0; e < kCols; e += 8) {
+                        uint4 w;
+                        __nv_bfloat162 *h = reinterpret_cast<__nv_bfloat162 *>(&w);
 #pragma unroll
-                        for (int e = 0; e < D / 8; e += 8) {
-                            uint4 w;
-                            __nv_bfloat162 *h = reinterpret_cast<__nv_bfloat162 *>(&w);
-#pragma unroll
-                            for (int z = 0; z < 4; ++z)
-                                h[z] = __floats2bfloat162_rn(acc[e + 2 * z][2 * x + y] * k, acc[e + 2 * z + 1][2 * x + y] * k);
-                            *reinterpret_cast<uint4 *>(to + y * (D / 8) + e) = w;
-                        }
-                    if (a.lse && c == 0)
-                        a.lse[o] = nan ? k : sum_l[x] == 0.f ? -INFINITY : (m[x] + log2f(sum_l[x])) * kAtLn2;
+                        for (int z = 0; z < 4; ++z) h[z] = __floats2bfloat162_rn(value(x, e + 2 * z) * k, value(x, e + 2 * z + 1) * k);
+                        *reinterpret_cast<uint4 *>(to + e) = w;
+                    }
+                    if (a.lse && lead) a.lse[o] = nan ? k : sum_l[x] == 0.f ? -INFINITY : (m[x] + log2f(sum_l[x])) * kAtLn2;
                 } else {
-                    float *to = part + ((int64_t)slot * kArRows + r) * D + c * (D / 4);
+                    const int slot = 2 * blockIdx.x + (first == 0 ? 1 : 0);
+                    float *to = part + ((int64_t)slot * kArRows + r) * D + col;
 #pragma unroll
-                    for (int y = 0; y < 2; ++y)
-#pragma unroll
-                        for (int e = 0; e < D / 8; e += 4)
-                            *reinterpret_cast<float4 *>(to + y * (D / 8) + e) =
-                                make_float4(acc[e][2 * x + y], acc[e + 1][2 * x + y], acc[e + 2][2 * x + y], acc[e + 3][2 * x + y]);
-                    if (c == 0) part_ml[(int64_t)slot * kArRows + r] = make_float2(m[x], sum_l[x]);
+                    for (int e = 0; e < kCols; e += 4)
+                        *reinterpret_cast<float4 *>(to + e) = make_float4(value(x, e), value(x, e + 1), value(x, e + 2), value(x, e + 3));
+                    if (lead) part_ml[(int64_t)slot * kArRows + r] = make_float2(m[x], sum_l[x]);
                 }
             }
         }
@@ -505,11 +636,11 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
             // a tile that begins here and goes on: the CTAs behind that have the rest of its blocks
             const int rest = at.blocks - steps;
             const bool goes_on = first == 0 && rest > 0;
-            join[blockIdx.x] = goes_on ? make_int4(at.row0, at.head, at.tile * kArRows | min(rows - at.tile * kArRows, kArRows) << 26,
+            join[blockIdx.x] = goes_on ? make_int4(at.row0, at.head, at.tile * R | min(rows - at.tile * R, R) << 26,
                                                    1 + (rest + chunk - 1) / chunk)
                                        : make_int4(0, 0, 0, 0);
         }
-        at.next(a, steps);
+        at.next<R>(a, steps);
     }
 }
 
