@@ -137,8 +137,9 @@ page_map_kernel(const int32_t *__restrict__ offsets, const int32_t *__restrict__
 //
 // A unit is (run, head, keys or values): the run are rows whose slots follow one another in one page, found from the
 // slots alone (a row leads a run if it starts a page, or the row ahead is not its page's token before it).  A CTA
-// takes the runs that begin in its window of rows; its threads hold the run in registers between the maximum and the
-// codes, so that it is read once.  Bound by HBM: 2 or 4 bytes read and 1 written an element.
+// takes the runs that begin in its window of rows, which it finds in one look at the slots (a bit per row that begins or ends
+// something); its threads hold the run in registers between the maximum and the codes, so that it is read once.
+// Bound by HBM: 2 or 4 bytes read and 1 written an element.
 constexpr int kCwThreads = 128;
 constexpr int kCwKeep = 8;                   // 16-byte vectors of a run that a thread keeps; longer runs are read twice
 constexpr int kCwMaxWindow = 64;
@@ -162,112 +163,145 @@ template <> struct CodesOf<float> {
     using Out = uint32_t;
 };
 
-// Codes of four values, x / s clamped to +-127 (s a power of two; inv = 1 / s).
+// Codes of four values of at most 127 s: x / s (inv = 1 / s, a power of two) added to 1.5 2^23 leaves the nearest whole number, ties to
+// even, in the sum's last bits, in two's complement.
 __device__ inline uint32_t codes4(float a, float b, float c, float d, float inv)
 {
-    const int i0 = __float2int_rn(fminf(fmaxf(a * inv, -127.f), 127.f)), i1 = __float2int_rn(fminf(fmaxf(b * inv, -127.f), 127.f));
-    const int i2 = __float2int_rn(fminf(fmaxf(c * inv, -127.f), 127.f)), i3 = __float2int_rn(fminf(fmaxf(d * inv, -127.f), 127.f));
-    return (uint32_t)(i0 & 255) | (uint32_t)(i1 & 255) << 8 | (uint32_t)(i2 & 255) << 16 | (uint32_t)i3 << 24;
+    constexpr float kRound = 12582912.f;
+    const uint32_t i0 = __float_as_uint(fmaf(a, inv, kRound)), i1 = __float_as_uint(fmaf(b, inv, kRound));
+    const uint32_t i2 = __float_as_uint(fmaf(c, inv, kRound)), i3 = __float_as_uint(fmaf(d, inv, kRound));
+    return __byte_perm(__byte_perm(i0, i1, 0x0040), __byte_perm(i2, i3, 0x0040), 0x5410);
 }
+// Four codes at a scale, to another.
+__device__ inline uint32_t shift4(uint32_t x, float shrink)
+{
+    return codes4((float)(int8_t)x, (float)(int8_t)(x >> 8), (float)(int8_t)(x >> 16), (float)(int8_t)(x >> 24), shrink);
+}
+// The largest |x| of a 16-byte vector, with what there was (NaN if there is one): in bf16 two at a time, on the bits.
+template <typename T> struct Largest;
+template <> struct Largest<__nv_bfloat16> {
+    uint32_t m = 0u;
+    __device__ static inline uint32_t max2(uint32_t a, uint32_t b)
+    {
+        uint32_t r;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    __device__ inline void take(const uint4 &v)
+    {
+        m = max2(m, max2(max2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), max2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
+    }
+    __device__ inline float value() const { return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u)); }
+};
+template <> struct Largest<float> {
+    float m = 0.f;
+    __device__ inline void take(const uint4 &v)
+    {
+        m = max_nan(m, max_nan(max_nan(fabsf(__uint_as_float(v.x)), fabsf(__uint_as_float(v.y))), max_nan(fabsf(__uint_as_float(v.z)), fabsf(__uint_as_float(v.w)))));
+    }
+    __device__ inline float value() const { return m; }
+};
 
 template <typename T>
-__global__ void __launch_bounds__(kCwThreads)
+__global__ void __launch_bounds__(kCwThreads, 8)
 cache_write_kernel(const T *__restrict__ k, int64_t k_stride, const T *__restrict__ v, int64_t v_stride, int rows, int window,
-                   const int32_t *__restrict__ slots, CacheView c)
+                   const int32_t *__restrict__ slots, const __grid_constant__ CacheView c)
 {
-    constexpr int kVec = Elem<T>::kPerVec;
+    constexpr int kVec = Elem<T>::kPerVec, kLook = (kCwMaxWindow + 128) / kCwThreads + 1;
     using Out = typename CodesOf<T>::Out;
-    __shared__ int lead[kCwMaxWindow], n_lead, stop;
-    __shared__ float red[kCwThreads / 32];
+    __shared__ uint32_t breaks[kLook * kCwThreads / 32], leads[kCwMaxWindow / 32];    // rows that do not follow the one ahead; those that lead a run
+    __shared__ int32_t slot_of[kCwMaxWindow];
+    __shared__ float red[2][kCwThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int head = blockIdx.y % c.kv_heads;
-    const bool values = (int)blockIdx.y >= c.kv_heads;
+    // the heads of a window beside each other: what runs at a time reads whole rows
+    const int units = 2 * c.kv_heads, unit = (int)(blockIdx.x % units);
+    const int row0 = (int)(blockIdx.x / units) * window, ps = c.page_size;
+    const int64_t n_slots = (int64_t)c.num_pages << c.page_shift;
+    ptx::grid_dep_launch();
+    ptx::grid_dep_wait();
+    // a run that begins in the window ends, at the latest, a page behind it
+    for (int i = tid; i < (window + ps + 31) / 32 * 32; i += kCwThreads) {
+        const int r = row0 + i;
+        const int s = r < rows ? __ldg(slots + r) : -1, ahead = r > 0 && r < rows ? __ldg(slots + r - 1) : -1;
+        const bool valid = s >= 0 && s < n_slots, follows = valid && (s & (ps - 1)) != 0 && ahead == s - 1;
+        const uint32_t brk = __ballot_sync(0xffffffffu, !follows), led = __ballot_sync(0xffffffffu, !follows && valid && i < window);
+        if (lane == 0) breaks[i >> 5] = brk;
+        if (lane == 0 && i < kCwMaxWindow) leads[i >> 5] = led;
+        if (i < kCwMaxWindow) slot_of[i] = s;
+    }
+    __syncthreads();
+    const int per_row = c.dim / kVec, row_step = kCwThreads / per_row;      // threads of a row; rows at a time
+    const int my_row = tid / per_row, my_vec = tid - my_row * per_row;
+    int turn = 0;
+    const bool values = unit >= c.kv_heads;
+    const int head = values ? unit - c.kv_heads : unit;
     const T *src = (values ? v : k) + (int64_t)head * c.dim;
     const int64_t stride = values ? v_stride : k_stride;
     int8_t *codes = values ? c.v : c.k;
     float *scales = values ? c.v_scale : c.k_scale;
-    const int row0 = (int)blockIdx.x * window, ps = c.page_size;
-    const int64_t n_slots = (int64_t)c.num_pages << c.page_shift;
-    if (tid == 0) n_lead = 0;
-    ptx::grid_dep_launch();
-    ptx::grid_dep_wait();
-    __syncthreads();
-    if (tid < window && row0 + tid < rows) {
-        const int r = row0 + tid, s = __ldg(slots + r);
-        if (s >= 0 && s < n_slots && ((s & (ps - 1)) == 0 || r == 0 || __ldg(slots + r - 1) != s - 1)) lead[atomicAdd(&n_lead, 1)] = r;
-    }
-    __syncthreads();
-    const int n = n_lead;
-    const int per_row = c.dim / kVec, row_step = kCwThreads / per_row;      // threads of a row; rows at a time
-    const int my_row = tid / per_row, my_vec = tid % per_row;
-    for (int u = 0; u < n; ++u) {
-        const int r0 = lead[u], slot0 = __ldg(slots + r0), at = slot0 & (ps - 1), page = slot0 >> c.page_shift;
-        if (tid == 0) stop = ps - at;
-        __syncthreads();
-        // the run's length: up to the first row that is not the slot's follower (a page has at most kCwThreads tokens)
-        if (tid < ps - at && (r0 + tid >= rows || __ldg(slots + r0 + tid) != slot0 + tid)) atomicMin(&stop, tid);
-        __syncthreads();
-        const int len = stop;
-        uint4 held[kCwKeep];
-        float top = 0.f;
+#pragma unroll 1
+    for (int word = 0; word * 32 < window; ++word)
+#pragma unroll 1
+        for (uint32_t left = leads[word]; left; left &= left - 1, turn ^= 1) {
+            const int i = word * 32 + __ffs(left) - 1, slot0 = slot_of[i], at = slot0 & (ps - 1), page = slot0 >> c.page_shift;
+            int next = (i + 1) >> 5;
+            uint32_t bits = breaks[next] & (0xffffffffu << ((i + 1) & 31));
+            while (!bits) bits = breaks[++next];                 // (there is one: where the page ends)
+            const int len = next * 32 + __ffs(bits) - 1 - i;
+            const T *from = src + (int64_t)(row0 + i + my_row) * stride + my_vec * kVec;
+            const int64_t step = row_step * stride;
+            float *scale = scales + (int64_t)page * c.kv_heads + head;
+            uint4 held[kCwKeep];
 #pragma unroll
-        for (int t = 0; t < kCwKeep; ++t) {
-            const int r = t * row_step + my_row;
-            held[t] = make_uint4(0u, 0u, 0u, 0u);
-            if (r < len) held[t] = __ldg(reinterpret_cast<const uint4 *>(src + (r0 + r) * stride) + my_vec);
-        }
-#pragma unroll
-        for (int t = 0; t < kCwKeep; ++t) {
-            float f[kVec];
-            Elem<T>::unpack(held[t], f);
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) top = max_nan(top, fabsf(f[e]));
-        }
-        for (int r = kCwKeep * row_step + my_row; r < len; r += row_step) {
-            float f[kVec];
-            Elem<T>::unpack(__ldg(reinterpret_cast<const uint4 *>(src + (r0 + r) * stride) + my_vec), f);
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) top = max_nan(top, fabsf(f[e]));
-        }
-        top = warp_max_redux(top);
-        if (lane == 0) red[warp] = top;
-        __syncthreads();
-        top = max_nan(max_nan(red[0], red[1]), max_nan(red[2], red[3]));
-        float *scale = scales + (int64_t)page * c.kv_heads + head;
-        const float old = at ? *scale : 0.f;
-        const float s = max_nan(block_scale(top), old);
-        const float inv = s > 0.f ? 1.f / s : 0.f;                // (NaN: codes 0)
-        int8_t *block = codes + ((int64_t)page * c.kv_heads + head) * ps * c.dim;
-        if (at && s != old && s == s) {
-            // the page's earlier codes, to the new scale
-            const float shrink = old * inv;
-            uint4 *p = reinterpret_cast<uint4 *>(block);
-            for (int i = tid; i < at * c.dim / 16; i += kCwThreads) {
-                uint4 w = p[i];
-                uint32_t *x = &w.x;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    x[e] = codes4((float)(int8_t)x[e], (float)(int8_t)(x[e] >> 8), (float)(int8_t)(x[e] >> 16), (float)(int8_t)(x[e] >> 24), shrink);
-                p[i] = w;
+            for (int t = 0; t < kCwKeep; ++t) {
+                held[t] = make_uint4(0u, 0u, 0u, 0u);
+                if (t * row_step + my_row < len) held[t] = __ldg(reinterpret_cast<const uint4 *>(from + t * step));
             }
+            const float old = at ? *scale : 0.f;
+            Largest<T> largest;
+#pragma unroll
+            for (int t = 0; t < kCwKeep; ++t) largest.take(held[t]);
+            for (int r = kCwKeep * row_step + my_row; r < len; r += row_step)
+                largest.take(__ldg(reinterpret_cast<const uint4 *>(from + (r - my_row) * stride)));
+            float top = largest.value();
+            top = warp_max_redux(top);
+            if (lane == 0) red[turn][warp] = top;
+            __syncthreads();
+            top = max_nan(max_nan(red[turn][0], red[turn][1]), max_nan(red[turn][2], red[turn][3]));
+            const float s = max_nan(block_scale(top), old);
+            const float inv = s > 0.f ? 1.f / s : 0.f;            // (NaN: codes 0)
+            int8_t *block = codes + ((int64_t)page * c.kv_heads + head) * ps * c.dim;
+            if (at && s != old && s == s) {
+                // the page's earlier codes, to the new scale
+                const float shrink = old * inv;
+                uint4 *p = reinterpret_cast<uint4 *>(block);
+                for (int j = tid; j < at * c.dim / 16; j += kCwThreads) {
+                    uint4 w = p[j];
+                    w.x = shift4(w.x, shrink);
+                    w.y = shift4(w.y, shrink);
+                    w.z = shift4(w.z, shrink);
+                    w.w = shift4(w.w, shrink);
+                    p[j] = w;
+                }
+            }
+            int8_t *to = block + (int64_t)(at + my_row) * c.dim + my_vec * kVec;
+            auto put = [&](int r, const uint4 &x) {
+                float f[kVec];
+                Elem<T>::unpack(x, f);
+                Out o;
+                uint32_t *w = reinterpret_cast<uint32_t *>(&o);
+#pragma unroll
+                for (int e = 0; e < kVec; e += 4) w[e / 4] = inv > 0.f ? codes4(f[e], f[e + 1], f[e + 2], f[e + 3], inv) : 0u;
+                *reinterpret_cast<Out *>(to + r * c.dim) = o;
+            };
+#pragma unroll
+            for (int t = 0; t < kCwKeep; ++t)
+                if (t * row_step + my_row < len) put(t * row_step, held[t]);
+            for (int r = kCwKeep * row_step; r + my_row < len; r += row_step) put(r, __ldg(reinterpret_cast<const uint4 *>(from + (int64_t)r * stride)));
+            // (every thread has its `old`: the barrier above lies between that and this; the next run has another page, and its maxima the other half
+            // of `red`)
+            if (tid == 0) *scale = s;
         }
-        auto put = [&](int r, const uint4 &x) {
-            float f[kVec];
-            Elem<T>::unpack(x, f);
-            Out o;
-            uint32_t *w = reinterpret_cast<uint32_t *>(&o);
-#pragma unroll
-            for (int e = 0; e < kVec; e += 4) w[e / 4] = inv > 0.f ? codes4(f[e], f[e + 1], f[e + 2], f[e + 3], inv) : 0u;
-            reinterpret_cast<Out *>(block + (int64_t)(at + r) * c.dim)[my_vec] = o;
-        };
-#pragma unroll
-        for (int t = 0; t < kCwKeep; ++t)
-            if (t * row_step + my_row < len) put(t * row_step + my_row, held[t]);
-        for (int r = kCwKeep * row_step + my_row; r < len; r += row_step)
-            put(r, __ldg(reinterpret_cast<const uint4 *>(src + (r0 + r) * stride) + my_vec));
-        __syncthreads();                                          // every thread has read the old scale, and `red`
-        if (tid == 0) *scale = s;
-    }
 }
 
 static int sm_count()
@@ -286,7 +320,9 @@ static cudaError_t launch_write(cudaStream_t st, const void *k, int64_t k_stride
     const int64_t want = (int64_t)rows * 2 * c.kv_heads / ((int64_t)sms * 8) + 1;
     int window = 1;
     while (window < kCwMaxWindow && window < want) window *= 2;
-    const dim3 grid((unsigned)((rows + window - 1) / window), (unsigned)(2 * c.kv_heads));
+    const int64_t ctas = (int64_t)((rows + window - 1) / window) * 2 * c.kv_heads;
+    if (ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
+    const dim3 grid((unsigned)ctas);
     return launch_chained(cache_write_kernel<T>, grid, dim3(kCwThreads), (size_t)0, st, (const T *)k, k_stride, (const T *)v, v_stride,
                           rows, window, slots, c);
 }
