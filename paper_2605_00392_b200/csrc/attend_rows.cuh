@@ -16,6 +16,7 @@
 // The work, all (request, kv head, tile of rows) with their blocks of 64 tokens, is one line that is cut into equal runs, one per CTA
 // (two to an SM), whatever the requests' lengths: each CTA sums up the batch for itself and finds its place.  A tile that a cut goes through is
 // left in parts (fp32 sums, m', l) that attend_join_kernel puts together in the order of the line, so results do not depend on timing.
+// Where every tile has a CTA of its own and few blocks, each CTA takes its tile whole, and there is nothing to join.
 // The ring runs across tiles: the next one's codes are on their way while this one's warps are added up.
 #pragma once
 #include "attend.cuh"
@@ -28,6 +29,7 @@ constexpr int kArBlock = 16 * kArWarps;              // tokens of a step
 constexpr int kArMostCtas = 3 * 160;                 // what the workspace is sized for (a B200 has 148 SMs)
 constexpr int kArRows = 16;
 constexpr int kArLeast = 4;                          // blocks of a run at least
+constexpr int kArWhole = 8;                          // blocks of the longest tile up to which tiles are taken whole
 
 template <int D, int R> struct ArShape {
     // CTAs of an SM (with 16 rows three would leave a thread 128 registers, which spill: no kernel here may have a stack frame)
@@ -71,22 +73,22 @@ struct ArPlace {
     }
 };
 
-template <int R> __device__ inline int64_t ar_units(const AttendArgs &a, int i)
+template <int R> __device__ inline int64_t ar_units(const AttendArgs &a, int i, bool whole)
 {
     int row0, n, len;
     if (!attend_request(a, i, row0, n, len)) return 0;
-    return (int64_t)((n * a.group + R - 1) / R) * a.c.kv_heads * max(1, (len + kArBlock - 1) / kArBlock);
+    return (int64_t)((n * a.group + R - 1) / R) * a.c.kv_heads * (whole ? 1 : max(1, (len + kArBlock - 1) / kArBlock));
 }
 
-// Where CTA `blockIdx.x` of the line begins, and how many blocks it takes (0: none).
-template <int R> __device__ inline int ar_find(const AttendArgs &a, ArPlace &at, int &chunk)
+// Where CTA `blockIdx.x` of the line begins, and how many blocks it takes (0: none).  whole: it takes the tile of that number.
+template <int R> __device__ inline int ar_find(const AttendArgs &a, bool whole, ArPlace &at, int &chunk)
 {
     __shared__ int64_t warp_units[kArWarps + 1], found_before;
     __shared__ int found;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (a.batch + kArThreads - 1) / kArThreads, i0 = min(tid * per, a.batch), i1 = min(i0 + per, a.batch);
     int64_t mine = 0;
-    for (int i = i0; i < i1; ++i) mine += ar_units<R>(a, i);
+    for (int i = i0; i < i1; ++i) mine += ar_units<R>(a, i, whole);
     int64_t upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -101,19 +103,24 @@ template <int R> __device__ inline int ar_find(const AttendArgs &a, ArPlace &at,
         if (w < warp) before += warp_units[w];
         total += warp_units[w];
     }
-    const int64_t run = max((total + gridDim.x - 1) / gridDim.x, (int64_t)kArLeast);
+    const int64_t run = whole ? 1 : max((total + gridDim.x - 1) / gridDim.x, (int64_t)kArLeast);
     const int64_t start = run * blockIdx.x;
     chunk = (int)run;
     if (start >= total) return 0;
     if (start >= before && start < before + mine) {
         int i = i0;
-        for (int64_t u; (u = ar_units<R>(a, i)) <= start - before; ++i) before += u;
+        for (int64_t u; (u = ar_units<R>(a, i, whole)) <= start - before; ++i) before += u;
         found = i;
         found_before = before;
     }
     __syncthreads();
     at.request<R>(a, found);
     const int64_t rel = start - found_before;
+    if (whole) {
+        at.tile = (int)(rel % at.tiles);
+        at.head = (int)(rel / at.tiles);
+        return at.blocks;
+    }
     at.block = (int)(rel % at.blocks);
     at.tile = (int)(rel / at.blocks % at.tiles);
     at.head = (int)(rel / at.blocks / at.tiles);
@@ -174,7 +181,7 @@ __device__ inline uint32_t mat_trans(uint32_t x)
 // (first row of the request, kv head, the tile's first row | its rows << 26, CTAs that it goes through; 0: there is none).
 template <int D, int R>
 __global__ void __launch_bounds__(kArThreads, ArShape<D, R>::kPerSm)
-attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ part, float2 *__restrict__ part_ml, int4 *__restrict__ join)
+attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float *__restrict__ part, float2 *__restrict__ part_ml, int4 *__restrict__ join)
 {
     using S = ArShape<D, R>;
     extern __shared__ uint8_t smem_raw[];
@@ -197,9 +204,9 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
     ptx::grid_dep_wait();
     ArPlace at;
     int chunk;
-    const int todo = ar_find<R>(a, at, chunk);          // (its barriers order the initialisation too)
+    const int todo = ar_find<R>(a, whole_tiles, at, chunk);          // (its barriers order the initialisation too)
     if (todo == 0) {
-        if (tid == 0) join[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (tid == 0 && !whole_tiles) join[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
 
@@ -632,7 +639,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, float *__restrict__ par
             }
         }
         left -= steps;
-        if (left == 0 && tid == 0) {
+        if (left == 0 && tid == 0 && !whole_tiles) {
             // a tile that begins here and goes on: the CTAs behind that have the rest of its blocks
             const int rest = at.blocks - steps;
             const bool goes_on = first == 0 && rest > 0;
