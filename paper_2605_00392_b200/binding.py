@@ -394,45 +394,62 @@ class PageMap(NamedTuple):
 
 
 _CODE = {torch.bfloat16: BF16, torch.float32: FP32}
+_I32, _F32, _F64, _BF, _I8 = torch.int32, torch.float32, torch.float64, torch.bfloat16, torch.int8
+
+# These calls are a few microseconds each, of which the checks below are a good part: shapes and strides are taken once, devices
+# compared by number.
 
 
-def _on_device(device: torch.device, stream: Optional[torch.cuda.Stream], where: str, call, *args) -> None:
-    """call(stream handle, *args) with `device` current."""
-    if device.index == torch._C._cuda_getDevice():
-        _check(call(_stream_handle(stream), *args), where)
+def _on_device(dev: int, stream: Optional[torch.cuda.Stream], where: str, call, *args) -> None:
+    """call(stream handle, *args) with device number `dev` current."""
+    if dev == torch._C._cuda_getDevice():
+        status = call(torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream, *args)
     else:
-        with torch.cuda.device(device):
-            _check(call(_stream_handle(stream), *args), where)
+        with torch.cuda.device(dev):
+            status = call(_stream_handle(stream), *args)
+    if status:
+        raise RtpruneError(status, where)
 
 
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
-
-
-def _int32(t: torch.Tensor, n: int, device: torch.device, what: str) -> int:
-    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < n or t.device != device:
-        raise ValueError("%s must be a contiguous int32 tensor of at least %d on %s" % (what, n, device))
+def _int32(t: torch.Tensor, n: int, dev: int, what: str) -> int:
+    if t.dtype is not _I32 or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor of at least %d on CUDA device %d" % (what, n, dev))
     return t.data_ptr()
 
 
-def _heads(t: torch.Tensor, rows: int, device: torch.device, what: str) -> int:
-    """Row stride, in elements, of [rows, heads, head_dim] with heads back to back."""
-    if t.dim() != 3 or t.shape[0] != rows or t.device != device or (rows and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]))):
-        raise ValueError("%s must be [%d, heads, head_dim] on %s, the heads of a row back to back" % (what, rows, device))
-    return t.stride(0) if rows > 1 else t.shape[1] * t.shape[2]
+def _heads(t: torch.Tensor, dtype: torch.dtype, rows: int, dim: int, dev: int, what: str):
+    """(heads, row stride in elements) of [rows, heads, head_dim] with heads back to back."""
+    shape = t.shape
+    if t.dtype is dtype and len(shape) == 3 and t.get_device() == dev:
+        r, heads, d = shape
+        row, head, one = t.stride()
+        if r == rows and d == dim and (rows == 0 or heads == 0 or (one == 1 and (head == d or heads == 1))):
+            return heads, row if rows > 1 else heads * d
+    raise ValueError("%s must be %s [%d, heads, %d] on CUDA device %d, the heads of a row back to back" % (what, dtype, rows, dim, dev))
 
 
-def _ccache(cache) -> CCache:
+def _tables(t: torch.Tensor, batch: int, dev: int):
+    """(address, row stride, entries of a row) of block tables."""
+    shape = t.shape
+    if t.dtype is _I32 and len(shape) == 2 and shape[0] == batch and t.get_device() == dev:
+        row, one = t.stride()
+        if one == 1 or shape[1] <= 1:
+            return t.data_ptr(), row if batch > 1 else shape[1], shape[1]
+    raise ValueError("block_tables must be int32 [%d, max_pages] on CUDA device %d, the entries of a row back to back" % (batch, dev))
+
+
+def _cache_of(cache):
+    """(device number, kv_heads, head_dim, rtprune_cache_t) of four tensors like a PagedCache's."""
     k, v, ks, vs = cache
-    if (k.dim() != 4 or k.shape != v.shape or k.dtype != torch.int8 or v.dtype != torch.int8 or not k.is_contiguous()
-            or not v.is_contiguous() or ks.dtype != torch.float32 or vs.dtype != torch.float32 or ks.shape != k.shape[:2]
-            or vs.shape != ks.shape or not ks.is_contiguous() or not vs.is_contiguous()
-            or not k.is_cuda or v.device != k.device or ks.device != k.device or vs.device != k.device):
-        raise ValueError("a cache is int8 codes k, v [pages, kv_heads, page_size, head_dim] and float32 scales [pages, kv_heads], "
-                         "contiguous, on one CUDA device")
-    pages, heads, page, dim = k.shape
-    return CCache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, page, heads, dim)
+    shape, dev = k.shape, k.get_device()
+    if len(shape) == 4:
+        pages, heads, page, dim = shape
+        if (k.dtype is _I8 and v.dtype is _I8 and ks.dtype is _F32 and vs.dtype is _F32 and v.shape == shape and ks.shape == (pages, heads)
+                and vs.shape == (pages, heads) and dev >= 0 and v.get_device() == dev and ks.get_device() == dev and vs.get_device() == dev
+                and k.is_contiguous() and v.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()):
+            return dev, heads, dim, CCache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, page, heads, dim)
+    raise ValueError("a cache is int8 codes k, v [pages, kv_heads, page_size, head_dim] and float32 scales [pages, kv_heads], "
+                     "contiguous, on one CUDA device")
 
 
 def rope_frequencies(rotary_dim: int, theta: float, device) -> torch.Tensor:
@@ -447,18 +464,16 @@ def map_pages(offsets: torch.Tensor, block_tables: torch.Tensor, free_pages: tor
     `token_index` are a run's out_offsets and kept_idx; `block_tables` [batch, max_pages] gets the new pages' entries; `out` is a
     PageMap (or four tensors like it), of as many rows as `out.slot_map` has."""
     slots, positions, lens, state = out
-    dev, batch = offsets.device, offsets.numel() - 1
-    _need(offsets.is_cuda and batch >= 0, "offsets must be [batch + 1] on a CUDA device")
-    rows = slots.numel()
-    _need(block_tables.dtype == torch.int32 and block_tables.dim() == 2 and block_tables.shape[0] == batch and block_tables.device == dev
-          and (block_tables.shape[1] <= 1 or block_tables.stride(1) == 1), "block_tables must be int32 [batch, max_pages], rows contiguous")
-    pages = block_tables.shape[1]
-    _on_device(dev, stream, "rtprune_page_map", lib().rtprune_page_map, _int32(offsets, batch + 1, dev, "offsets"),
+    dev, batch, rows = offsets.get_device(), offsets.numel() - 1, slots.numel()
+    if dev < 0 or batch < 0:
+        raise ValueError("offsets must be [batch + 1] on a CUDA device")
+    table, table_stride, pages = _tables(block_tables, batch, dev)
+    _on_device(dev, stream, "rtprune_page_map", lib().rtprune_page_map, _int32(offsets, 0, dev, "offsets"),
                None if context_lens is None else _int32(context_lens, batch, dev, "context_lens"), batch, rows,
                None if token_index is None else _int32(token_index, rows, dev, "token_index"),
                None if position_base is None else _int32(position_base, batch, dev, "position_base"),
                _int32(free_pages, 0, dev, "free_pages"), _int32(free_head, 1, dev, "free_head"), free_pages.numel(), page_size,
-               block_tables.data_ptr(), block_tables.stride(0) if batch > 1 else pages, pages, _int32(slots, 0, dev, "slot_map"),
+               table, table_stride, pages, _int32(slots, 0, dev, "slot_map"),
                None if positions is None else _int32(positions, rows, dev, "positions"), _int32(lens, batch, dev, "seq_lens"),
                _int32(state, 2, dev, "state"))
 
@@ -469,29 +484,44 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inv_
                  stream: Optional[torch.cuda.Stream] = None) -> None:
     """rtprune_qk_norm_rope on q [rows, q_heads, head_dim] and k [rows, kv_heads, head_dim] (bf16 or float32; rows may be parts of
     a fused projection's).  In place unless q_out, k_out are given.  The rotated part is 2 * inv_freq.numel() wide."""
-    dev, rows = q.device, q.shape[0]
-    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
-    dim, dtype = q.shape[-1], q.dtype
-    _need(q.is_cuda and dtype in _CODE, "q must be bf16 or float32 on a CUDA device")
-    for t in (k, q_out, k_out):
-        _need(t.dtype == dtype and t.shape[-1] == dim, "q, k and the outputs must have one dtype and head_dim")
-    _need(q_out.shape == q.shape and k_out.shape == k.shape, "the outputs must have the inputs' shapes")
+    dev, dtype, shape = q.get_device(), q.dtype, q.shape
+    if dev < 0 or dtype not in _CODE or len(shape) != 3:
+        raise ValueError("q must be bf16 or float32 [rows, q_heads, head_dim] on a CUDA device")
+    rows, _, dim = shape
+    q_heads, q_row = _heads(q, dtype, rows, dim, dev, "q")
+    k_heads, k_row = _heads(k, dtype, rows, dim, dev, "k")
+    qo, qo_row, ko, ko_row = q, q_row, k, k_row
+    if q_out is not None:
+        qo, (heads, qo_row) = q_out, _heads(q_out, dtype, rows, dim, dev, "q_out")
+        if heads != q_heads:
+            raise ValueError("q_out must have q's shape")
+    if k_out is not None:
+        ko, (heads, ko_row) = k_out, _heads(k_out, dtype, rows, dim, dev, "k_out")
+        if heads != k_heads:
+            raise ValueError("k_out must have k's shape")
     for w in (q_weight, k_weight):
-        _need(w is None or (w.dtype == dtype and w.numel() == dim and w.is_contiguous() and w.device == dev), "weights must be [head_dim] like q")
-    _need(inv_freq.dtype == torch.float64 and inv_freq.is_contiguous() and inv_freq.device == dev, "inv_freq must be contiguous float64 on q's device")
-    _on_device(dev, stream, "rtprune_qk_norm_rope", lib().rtprune_qk_norm_rope, _CODE[dtype], q.data_ptr(), _heads(q, rows, dev, "q"),
-               k.data_ptr(), _heads(k, rows, dev, "k"), rows, q.shape[1], k.shape[1], dim, _ptr(q_weight), _ptr(k_weight), eps,
-               _int32(positions, rows, dev, "positions"), inv_freq.data_ptr(), 2 * inv_freq.numel(), int(interleaved),
-               q_out.data_ptr(), _heads(q_out, rows, dev, "q_out"), k_out.data_ptr(), _heads(k_out, rows, dev, "k_out"))
+        if w is not None and (w.dtype is not dtype or w.numel() != dim or w.get_device() != dev or not w.is_contiguous()):
+            raise ValueError("weights must be [head_dim], of q's dtype and device")
+    if inv_freq.dtype is not _F64 or inv_freq.get_device() != dev or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq must be contiguous float64 on q's device")
+    _on_device(dev, stream, "rtprune_qk_norm_rope", lib().rtprune_qk_norm_rope, _CODE[dtype], q.data_ptr(), q_row, k.data_ptr(), k_row, rows,
+               q_heads, k_heads, dim, None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+               eps, _int32(positions, rows, dev, "positions"), inv_freq.data_ptr(), 2 * inv_freq.numel(), interleaved, qo.data_ptr(), qo_row,
+               ko.data_ptr(), ko_row)
 
 
 def cache_write(k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, cache, *, stream: Optional[torch.cuda.Stream] = None) -> None:
     """rtprune_cache_write: k, v [rows, kv_heads, head_dim] (bf16 or float32) to the slots of a PagedCache; rows with slot -1 go nowhere."""
-    c, dev, rows = _ccache(cache), cache[0].device, k.shape[0]
-    _need(k.dtype in _CODE and v.dtype == k.dtype, "k and v must both be bf16 or both float32")
-    _need(k.shape == v.shape and k.shape[1:] == (c.kv_heads, c.head_dim), "k and v must be [rows, kv_heads, head_dim] of the cache")
-    _on_device(dev, stream, "rtprune_cache_write", lib().rtprune_cache_write, _CODE[k.dtype], k.data_ptr(), _heads(k, rows, dev, "k"),
-               v.data_ptr(), _heads(v, rows, dev, "v"), rows, _int32(slot_map, rows, dev, "slot_map"), c)
+    dev, heads, dim, c = _cache_of(cache)
+    dtype, rows = k.dtype, k.shape[0]
+    if dtype not in _CODE:
+        raise ValueError("k and v must both be bf16 or both float32")
+    k_heads, k_row = _heads(k, dtype, rows, dim, dev, "k")
+    v_heads, v_row = _heads(v, dtype, rows, dim, dev, "v")
+    if k_heads != heads or v_heads != heads:
+        raise ValueError("k and v must have the cache's %d heads" % heads)
+    _on_device(dev, stream, "rtprune_cache_write", lib().rtprune_cache_write, _CODE[dtype], k.data_ptr(), k_row, v.data_ptr(), v_row, rows,
+               _int32(slot_map, rows, dev, "slot_map"), c)
 
 
 def cache_attend(q: torch.Tensor, offsets: torch.Tensor, seq_lens: torch.Tensor, block_tables: torch.Tensor, cache, *, max_q_len: int,
@@ -502,31 +532,28 @@ def cache_attend(q: torch.Tensor, offsets: torch.Tensor, seq_lens: torch.Tensor,
     over the seq_lens[i] tokens that it has in the cache.  scale: head_dim^-1/2 unless given.  Returns `out` (bf16, zeros where no
     tensor was given); `lse` float32 [rows, q_heads] is filled if given.  `workspace`: cache_attend_workspace bytes of the caller's,
     else the call takes them from torch's allocator on its stream."""
-    c, dev, rows = _ccache(cache), cache[0].device, q.shape[0]
-    batch = offsets.numel() - 1
     if stream is not None and (out is None or workspace is None):
         with torch.cuda.stream(stream):        # memory taken here belongs to the stream that uses it
             return cache_attend(q, offsets, seq_lens, block_tables, cache, max_q_len=max_q_len, max_seq_len=max_seq_len, scale=scale,
                                 causal=causal, out=out, lse=lse, workspace=workspace)
-    _need(q.dtype == torch.bfloat16 and q.dim() == 3 and q.shape[2] == c.head_dim, "q must be bf16 [rows, q_heads, head_dim of the cache]")
-    stride, heads = _heads(q, rows, dev, "q"), q.shape[1]
+    dev, kv_heads, dim, c = _cache_of(cache)
+    rows, batch = q.shape[0], offsets.numel() - 1
+    heads, row = _heads(q, _BF, rows, dim, dev, "q")
     if out is None:
-        out = torch.zeros((rows, heads, c.head_dim), dtype=torch.bfloat16, device=dev)
-    _need(out.dtype == torch.bfloat16 and out.shape == q.shape and out.is_contiguous() and out.device == dev, "out must be contiguous bf16 of q's shape")
-    _need(lse is None or (lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous() and lse.device == dev),
-          "lse must be contiguous float32 [rows, q_heads]")
-    _need(block_tables.dtype == torch.int32 and block_tables.dim() == 2 and block_tables.shape[0] == batch and block_tables.device == dev
-          and (block_tables.shape[1] <= 1 or block_tables.stride(1) == 1), "block_tables must be int32 [batch, max_pages], rows contiguous")
+        out = torch.zeros((rows, heads, dim), dtype=_BF, device=q.device)
+    elif out.dtype is not _BF or out.get_device() != dev or out.shape != q.shape or not out.is_contiguous():
+        raise ValueError("out must be contiguous bf16 of q's shape")
+    if lse is not None and (lse.dtype is not _F32 or lse.get_device() != dev or lse.shape != (rows, heads) or not lse.is_contiguous()):
+        raise ValueError("lse must be contiguous float32 [rows, q_heads]")
+    table, table_stride, pages = _tables(block_tables, batch, dev)
     if workspace is None:
-        workspace = torch.empty(cache_attend_workspace(batch, max_q_len, max_seq_len, heads, c.kv_heads, c.head_dim),
-                                dtype=torch.uint8, device=dev)
-    _need(workspace.device == dev and workspace.is_contiguous(), "the workspace must be contiguous on the cache's device")
-    pages = block_tables.shape[1]
-    _on_device(dev, stream, "rtprune_cache_attend", lib().rtprune_cache_attend, q.data_ptr(), stride, rows, heads,
-               _int32(offsets, batch + 1, dev, "offsets"), _int32(seq_lens, batch, dev, "seq_lens"), batch, max_q_len, max_seq_len,
-               block_tables.data_ptr(), block_tables.stride(0) if batch > 1 else pages, pages, c,
-               c.head_dim ** -0.5 if scale is None else scale, int(causal), out.data_ptr(), _ptr(lse), workspace.data_ptr(),
-               workspace.numel() * workspace.element_size())
+        workspace = torch.empty(cache_attend_workspace(batch, max_q_len, max_seq_len, heads, kv_heads, dim), dtype=torch.uint8, device=q.device)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous on the cache's device")
+    _on_device(dev, stream, "rtprune_cache_attend", lib().rtprune_cache_attend, q.data_ptr(), row, rows, heads,
+               _int32(offsets, 0, dev, "offsets"), _int32(seq_lens, batch, dev, "seq_lens"), batch, max_q_len, max_seq_len, table, table_stride,
+               pages, c, dim ** -0.5 if scale is None else scale, causal, out.data_ptr(), None if lse is None else lse.data_ptr(),
+               workspace.data_ptr(), workspace.nbytes)
     return out
 
 

@@ -304,13 +304,6 @@ cache_write_kernel(const T *__restrict__ k, int64_t k_stride, const T *__restric
         }
 }
 
-static int sm_count()
-{
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    return sms;
-}
-
 template <typename T>
 static cudaError_t launch_write(cudaStream_t st, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int rows,
                                 const int32_t *slots, const CacheView &c, int sms)
@@ -375,7 +368,7 @@ extern "C" rtprune_status_t rtprune_cache_write(void *cuda_stream, rtprune_dtype
         ((uintptr_t)k | (uintptr_t)v) & 15u)
         return RTPRUNE_ERR_INVALID_ARG;
     if (rows > INT32_MAX - kCwMaxWindow) return RTPRUNE_ERR_UNSUPPORTED;
-    const int sms = sm_count();
+    const int sms = device_sms();
     if (!sms) return RTPRUNE_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const cudaError_t e = dtype == RTPRUNE_BF16 ? launch_write<__nv_bfloat16>(st, k, k_stride, v, v_stride, (int)rows, slot_map, c, sms)

@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/rtprune.h"
 #include "common.cuh"
 #include "ptx.cuh"
@@ -27,6 +29,18 @@ inline cudaError_t launch_chained(void (*kernel)(KArgs...), dim3 grid, dim3 bloc
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+// SMs of the current device, asked for once (0: no answer).
+inline int device_sms()
+{
+    static std::atomic<int> known[64];
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    if (dev < 64 && (sms = known[dev].load(std::memory_order_relaxed))) return sms;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    if (dev < 64) known[dev].store(sms, std::memory_order_relaxed);
+    return sms;
 }
 
 // Pages [num_pages][kv_heads][page_size][head_dim] of codes, scales [num_pages][kv_heads].
