@@ -408,14 +408,14 @@ rtprune_status_t rtprune_cache_write(void *cuda_stream, rtprune_dtype_t dtype, c
  * L_i = seq_lens[i] tokens, which are all in the cache: its row j sees tokens t <= L_i - n_i + j, or with causal = 0 all L_i.
  *   s_t = scale * (q . k_t),   out = sum_t softmax(s)_t v_t,   lse = log sum_t exp(s_t)
  * Query head h reads kv head h / (q_heads / kv_heads).  A row that sees nothing gives out = 0, lse = -inf.  A row that sees a block of
- * scale NaN, or whose query is not finite, gives NaN, and so does a row of a request that sees an entry of its table outside the cache or whose
+ * scale NaN, or whose query is not finite, gives NaN (an infinite query may also give 0 or the values of its largest scores), and so does a row of a request that sees an entry of its table outside the cache or whose
  * seq_lens is outside 0 .. max_seq_len.  A request of more than max_q_len rows is passed over.  Values agree with those formulas in 64 bits to
  * the rounding of bf16; the softmax and all sums are fp32.  What a row's result is does not depend on the call's timing.
  *
  *   q            DEVICE bf16 [rows] rows of q_heads heads of head_dim, 16-byte aligned, row stride in elements, a multiple of 8
  *   offsets      DEVICE int32 [batch+1], seq_lens DEVICE int32 [batch]; batch <= 65535
  *   max_q_len, max_seq_len  HOST upper bounds of n_i and L_i, max_seq_len <= max_pages * page_size; they choose the kernels and the
- *                grid, not the result
+ *                grid (and so how sums are put together), not what is computed
  *   block_tables DEVICE int32 [batch] rows, table_stride apart, of max_pages entries
  *   out          DEVICE bf16 [rows][q_heads][head_dim], 32-byte aligned; lse DEVICE float [rows][q_heads], may be NULL.
  *                Rows of no request are left as they are.

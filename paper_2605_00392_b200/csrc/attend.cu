@@ -9,10 +9,19 @@
 
 namespace rtp {
 
-constexpr int kAtFewRows = 64;               // rows of a kv head up to which attend_rows_kernel takes the call
+constexpr int kAtFewRows = 32, kAtFewTiles = 296;
 
-// Whether attend_rows_kernel takes the call: few rows, or more heads of a kv head than a tile has rows.
-static bool few_rows(int64_t max_q_len, int group) { return max_q_len * group <= kAtFewRows || group > kTlRows; }
+// Whether attend_rows_kernel takes the call: few rows of a kv head, so few tiles of 16 rows in the whole call that it has them all in one
+// go, two to an SM, where attend_tiles_kernel's of 256 rows leave most SMs without any, or more heads of a kv head than a tile has rows.
+// Rows against tiles, heads of 128, in us.  64 requests behind 1000 tokens, 10 heads: of 16 rows 52 / 108, 32 rows 93 / 112, 48 rows
+// 133 / 113, 128 rows 348 / 123; 16 requests behind 16000, 8 heads of 4: 32 rows 242 / 256, 64 rows 472 / 258.  Few tiles, 10 heads:
+// 220 (one image of 337 tokens) 10.7 / 13.2, 440 (two) 19.0 / 13.1, 320 (8 x 64 rows behind 1000) 31 / 29, 160 (2 x 128 behind 4000)
+// 47 / 82, 80 (128 behind 16000) 81 / 246.
+static bool few_rows(int64_t batch, int64_t max_q_len, int64_t kv_heads, int group)
+{
+    const int64_t rows = max_q_len * group;
+    return rows <= kAtFewRows || batch * kv_heads * ((rows + 15) / 16) <= kAtFewTiles || group > kTlRows;
+}
 
 // Workspace of attend_rows_kernel with `ctas` CTAs.
 struct RowsLayout {
@@ -75,7 +84,8 @@ static cudaError_t launch_rows(const AttendArgs &a, uint8_t *ws, cudaStream_t st
     if (!ctas) return cudaErrorInvalidDevice;
     const RowsLayout w = rows_layout(ctas, D);
     // every tile a CTA of its own, and a second kernel saved, where there are CTAs enough for as many as there can be and the longest is short.
-    // One request of 500 tokens, 28 heads on 4: 10.1 us on the GPU against 9.2 cut and joined, but a call from the host 18.8 us against 24.2.
+    // 10 heads, one token for one request of 256 tokens 6.9 us against 8.3 cut and joined, for one of 500 10.1 against 9.0 on the GPU but 18.8
+    // against 24.2 a call from the host, for 44 of 101 to 500 13.0 against 16.6; for one of 1001 16.7 against 10.4.
     const int64_t tiles = (int64_t)a.batch * a.c.kv_heads * (((int64_t)std::min(a.max_q_len, a.rows) * a.group + R - 1) / R);
     const bool whole = tiles <= ctas && a.max_len <= kArWhole * kArBlock;
     static std::atomic<unsigned long long> ready{0};             // devices that know the kernel's shared memory
@@ -118,7 +128,7 @@ extern "C" rtprune_status_t rtprune_cache_attend_workspace(int32_t batch, int32_
     if (!workspace_bytes || batch < 0 || max_q_len < 0 || max_seq_len < 0 || q_heads <= 0 || kv_heads <= 0 || head_dim <= 0)
         return RTPRUNE_ERR_INVALID_ARG;
     *workspace_bytes = 256;
-    if (rtp::few_rows(max_q_len, q_heads / kv_heads))
+    if (rtp::few_rows(batch, max_q_len, kv_heads, q_heads / kv_heads))
         *workspace_bytes = rtp::rows_layout(rtp::kArMostCtas, head_dim).total;
     return RTPRUNE_OK;
 }
@@ -151,9 +161,14 @@ extern "C" rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *
     AttendArgs a = {(const __nv_bfloat16 *)q, q_stride, offsets, seq_lens, block_tables, table_stride, batch, (int)rows, q_heads,
                     q_heads / c.kv_heads, max_q_len, (int)max_seq_len, max_pages, c, scale * 1.4426950408889634f, causal ? 1 : 0,
                     (__nv_bfloat16 *)out, lse};
-    if (few_rows(max_q_len, a.group)) {
+    if (few_rows(batch, max_q_len, c.kv_heads, a.group)) {
+        // a tile's first row has 26 bits of a word, and a CTA's blocks (of half a 148th of the line, and fewer) an int
+        const int64_t most = std::min<int64_t>(max_q_len, rows) * a.group, tiles = (most + 7) / 8 * batch * c.kv_heads;
+        if (most >= 1 << 26 || tiles * (max_seq_len / kArBlock + 1) / 64 > INT32_MAX) return RTPRUNE_ERR_UNSUPPORTED;
         uint8_t *ws = (uint8_t *)workspace;
         cudaStream_t st = (cudaStream_t)cuda_stream;
+        // tiles of 8 rows where a request has no more: 64 steps 37 us against 51 with 16, 16 long ones of 4 heads 116 against 153 (at 32 rows of
+        // a kv head, 16 requests behind 16000 tokens, 344 against 242)
         const bool eight = (int64_t)max_q_len * a.group <= 8;
         const cudaError_t e = c.dim == 128 ? eight ? launch_rows<128, 8>(a, ws, st) : launch_rows<128, 16>(a, ws, st)
                                            : eight ? launch_rows<64, 8>(a, ws, st) : launch_rows<64, 16>(a, ws, st);

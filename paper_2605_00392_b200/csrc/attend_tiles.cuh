@@ -27,7 +27,7 @@ constexpr int kTlTiles = 2;
 constexpr int kTlBlock = 128;                        // tokens of a block
 constexpr int kTlSoft = kTlTiles * kTlRows;
 constexpr int kTlThreads = kTlSoft + 128 + 128;     // (the last warp only makes it 128 registers a thread)
-constexpr int kTlSoftRegs = 176, kTlCodeRegs = 64, kTlOtherRegs = 96;    // registers of a thread: 2, 1, 1 of four warpgroups
+constexpr int kTlSoftRegs = 176, kTlCodeRegs = 56, kTlOtherRegs = 104;   // registers of a thread: 2, 1, 1 of four warpgroups
 static_assert(2 * kTlSoftRegs + kTlCodeRegs + kTlOtherRegs <= 4 * 128, "what the block was launched with");
 constexpr int kTlGroups = kTlBlock / 16;             // a page holds at least 16 tokens: scales are per 16
 

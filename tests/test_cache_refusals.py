@@ -90,6 +90,11 @@ def test_cache_attend_refusals():
         assert _attend(**bad) == INVALID, bad
     for bad in (dict(batch=65536), dict(heads=4098, qs=4098 * 128), dict(rows=2 ** 31)):
         assert _attend(**bad) == UNSUPPORTED, bad
+    one = dict(num_pages=1 << 17, kv_heads=1)             # more heads than a tile has rows: the tiles of few rows, counted in 26 bits
+    long = dict(num_pages=1 << 22, page_size=16, kv_heads=1)
+    assert _attend(_cache(**one), heads=256, qs=256 * 128, rows=1 << 18, batch=1, max_q=1 << 18) == UNSUPPORTED
+    assert _attend(_cache(**long), heads=256, qs=256 * 128, rows=1 << 17, batch=4096, max_q=1 << 17, max_len=1 << 26, pages=1 << 22,
+                   stride=1 << 22) == UNSUPPORTED
     for bad in (dict(ws=None), dict(ws=P + 16), dict(bytes=0)):
         assert _attend(**bad) == WORKSPACE, bad
     for kw, status in BAD_CACHES:

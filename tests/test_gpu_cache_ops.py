@@ -228,6 +228,19 @@ def _batch(new, lens, qh, kh, dim, page, seed, spare=2):
     return q.to(torch.bfloat16), _i32(np.concatenate([[0], np.cumsum(new)])), _i32(lens), tables, cache
 
 
+@pytest.fixture(params=[0, 6000], ids=["bounds", "loose"])
+def bounds(request, monkeypatch):
+    """max_q_len as the test has it, and far above: the bound chooses the kernel, so each test runs through both.  Gives what is added."""
+    attend, space = binding.cache_attend, binding.cache_attend_workspace
+
+    def loose(*args, max_q_len, **kw):
+        return attend(*args, max_q_len=max_q_len + request.param, **kw)
+
+    monkeypatch.setattr(binding, "cache_attend", loose)
+    monkeypatch.setattr(binding, "cache_attend_workspace", lambda batch, q, *rest: space(batch, q + request.param, *rest))
+    return request.param
+
+
 def _check_attend(q, offsets, lens, tables, cache, max_q, max_len, scale=None, causal=True, **kw):
     keep = 3.0
     out = torch.full(q.shape, keep, dtype=torch.bfloat16, device=DEV)
@@ -262,6 +275,7 @@ SHAPES = [
     ([260], [1300], 8, 2, 128, 32), ([700], [700], 2, 1, 64, 128), ([513], [2600], 1, 1, 128, 16), ([40, 41], [300, 41], 24, 3, 128, 16)]
 
 
+@pytest.mark.usefixtures("bounds")
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("new,lens,qh,kh,dim,page", SHAPES)
 def test_attend(new, lens, qh, kh, dim, page, causal):
@@ -269,6 +283,16 @@ def test_attend(new, lens, qh, kh, dim, page, causal):
     _check_attend(q, off, L, tables, cache, max(new), max(lens), causal=causal)
 
 
+@pytest.mark.usefixtures("bounds")
+@pytest.mark.parametrize("new,lens,qh,kh,dim,page", [
+    ([3, 40], [70, 300], 160, 1, 64, 16), ([2, 0, 1], [3000, 9, 1], 512, 2, 128, 64), ([40] * 40, [40 + i for i in range(40)], 8, 8, 64, 64),
+    ([40 - i for i in range(40)], [700 - 9 * i for i in range(40)], 8, 8, 128, 32), ([8] * 3, [2000, 8, 511], 1, 1, 128, 16), ([2] * 5, [513, 512, 511, 2, 5], 28, 4, 64, 64)])
+def test_attend_many_heads_and_tiles(new, lens, qh, kh, dim, page):
+    q, off, L, tables, cache = _batch(new, lens, qh, kh, dim, page, 31)
+    _check_attend(q, off, L, tables, cache, max(new), max(lens))
+
+
+@pytest.mark.usefixtures("bounds")
 @pytest.mark.parametrize("new,lens,qh,kh,dim,page", [([1, 1], [40, 700], 8, 2, 128, 64), ([9, 5], [200, 64], 4, 4, 64, 32), ([200, 130], [333, 130], 4, 2, 128, 64)])
 def test_attend_loose_bounds_strided_queries_and_scale(new, lens, qh, kh, dim, page):
     q, off, L, tables, cache = _batch(new, lens, qh, kh, dim, page, 11)
@@ -285,6 +309,7 @@ def test_attend_loose_bounds_strided_queries_and_scale(new, lens, qh, kh, dim, p
     assert (a[0][:n].float() - b[0][:n].float()).abs().max() <= 2 ** -6 * b[0][:n].float().abs().max()
 
 
+@pytest.mark.usefixtures("bounds")
 @pytest.mark.parametrize("new,lens,dim", [([4], [2], 64), ([6, 1], [3, 0], 128), ([300], [200], 128), ([140, 150], [0, 129], 64)])
 def test_attend_rows_that_see_nothing(new, lens, dim):
     # more queries than tokens: the first rows of a causal mask are empty
@@ -294,6 +319,7 @@ def test_attend_rows_that_see_nothing(new, lens, dim):
     assert (out[:gap] == 0).all() and torch.isneginf(lse[:gap]).all()
 
 
+@pytest.mark.usefixtures("bounds")
 @pytest.mark.parametrize("new,lens", [([1], [200]), ([5], [200]), ([150], [200])])
 def test_attend_scales_far_apart_zero_and_large_scores(new, lens):
     q, off, L, tables, cache = _batch(new, lens, 4, 2, 128, 16, 8)
@@ -310,6 +336,7 @@ def test_attend_scales_far_apart_zero_and_large_scores(new, lens):
     _check_attend(torch.zeros_like(q), off, L, tables, cache, max(new), max(lens))
 
 
+@pytest.mark.usefixtures("bounds")
 @pytest.mark.parametrize("new,lens", [([1], [200]), ([5], [200]), ([150], [200])])
 def test_attend_queries_of_every_size(new, lens):
     q, off, L, tables, cache = _batch(new, lens, 4, 2, 128, 64, 9)
@@ -320,7 +347,7 @@ def test_attend_queries_of_every_size(new, lens):
 
 
 @pytest.mark.parametrize("new,lens", [([1, 1], [100, 90]), ([6, 1], [100, 90]), ([90, 100], [100, 200])])
-def test_attend_not_finite_and_pages_outside(new, lens):
+def test_attend_not_finite_and_pages_outside(bounds, new, lens):
     q, off, L, tables, cache = _batch(new, lens, 2, 2, 64, 16, 4)
     clean = binding.cache_attend(q, off, L, tables, cache, max_q_len=max(new), max_seq_len=max(lens))
     last = int(L[0]) - 1
@@ -368,7 +395,7 @@ def test_attend_not_finite_and_pages_outside(new, lens):
         assert o[:new[0]].isnan().all()
         torch.testing.assert_close(o[new[0]:int(off[-1])], clean[new[0]:int(off[-1])], rtol=2 ** -6, atol=1e-3)
     # a request of more rows than max_q_len is passed over; so are rows outside the tensor
-    if new[0] > new[1]:
+    if new[0] > new[1] and bounds == 0:
         o = binding.cache_attend(q, off, L, tables, cache, max_q_len=new[1], max_seq_len=max(lens), out=torch.full_like(q, 2.0))
         assert (o[:new[0]] == 2).all()
     off2 = off.clone()
@@ -377,6 +404,7 @@ def test_attend_not_finite_and_pages_outside(new, lens):
     assert (o[new[0]:] == 2).all()
 
 
+@pytest.mark.usefixtures("bounds")
 @pytest.mark.parametrize("new,lens,qh,kh", [([1] * 5, [2000, 3, 900, 64, 4000], 8, 2), ([2, 3], [900, 40], 10, 10), ([300, 200], [400, 200], 4, 4)])
 def test_attend_twice_the_same_and_across_streams_and_graphs(new, lens, qh, kh):
     q, off, L, tables, cache = _batch(new, lens, qh, kh, 128, 64, 21)
@@ -412,6 +440,7 @@ def test_attend_twice_the_same_and_across_streams_and_graphs(new, lens, qh, kh):
         assert torch.equal(a[:n], o[:n])
 
 
+@pytest.mark.usefixtures("bounds")
 def test_attend_offsets_beyond_32_bits():
     # a cache of more than 2^31 elements: pages at its end
     page, kh, dim = 128, 16, 128
@@ -432,6 +461,51 @@ def test_attend_offsets_beyond_32_bits():
         a = binding.cache_attend(q, off, L, ids.view(1, -1), cache, max_q_len=n, max_seq_len=rows)
         b = binding.cache_attend(q, off, L, torch.arange(20, dtype=torch.int32, device=DEV).view(1, -1), small, max_q_len=n, max_seq_len=rows)
         assert torch.equal(a, b)
+
+
+# ---- on other streams and in graphs ------------------------------------------------------------------------------------
+
+def test_page_map_rope_and_write_in_a_graph_on_another_stream():
+    """The three captured together on a stream of their own and replayed for two batches: as the same calls one by one."""
+    new, ctx, page, kh, qh, dim, cap = [[5, 0, 130, 1], [1, 66, 2, 64]], [3, 64, 0, 127], 64, 2, 6, 64, 140
+    off = [np.concatenate([[0], np.cumsum(n)]) for n in new]
+    tables0 = torch.full((4, 6), -1, dtype=torch.int32, device=DEV)
+    for i, c in enumerate(ctx):
+        tables0[i, :-(-c // page)] = torch.arange(-(-c // page), device=DEV, dtype=torch.int32) + 10 + 3 * i
+    free, freq = torch.arange(30, 50, device=DEV, dtype=torch.int32), binding.rope_frequencies(dim, 1e4, DEV)
+    fused = [torch.randn(cap, (qh + 2 * kh) * dim, generator=torch.Generator(DEV).manual_seed(t), device=DEV).to(torch.bfloat16) for t in (0, 1)]
+
+    def state():
+        c = binding.PagedCache.allocate(60, kh, page, dim, DEV)
+        for t in c:
+            t.copy_(torch.randint(-99, 99, t.shape, generator=torch.Generator(DEV).manual_seed(7), device=DEV)) if t.dtype is torch.int8 else t.fill_(0.25)
+        return c, tables0.clone(), binding.PageMap.allocate(cap, 4, DEV), _i32(off[0]), fused[0].clone(), _i32([2]), _i32(ctx)
+
+    def calls(c, tables, m, offsets, x, head, lens, stream=None):
+        q, k, v = (t.unflatten(1, (-1, dim)) for t in x.split([qh * dim, kh * dim, kh * dim], 1))
+        binding.map_pages(offsets, tables, free, head, m, page_size=page, context_lens=lens, stream=stream)
+        binding.qk_norm_rope(q, k, m.positions, freq, stream=stream)
+        binding.cache_write(k, v, m.slot_map, c, stream=stream)
+
+    eager, side = state(), torch.cuda.Stream()
+    replayed = state()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        calls(*replayed, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    for t in (0, 1):
+        for s in (eager, replayed):
+            s[3].copy_(_i32(off[t]))
+            s[4].copy_(fused[t])
+        calls(*eager)
+        g.replay()
+        for a, b in zip((*eager[0], eager[1], *eager[2], eager[4]), (*replayed[0], replayed[1], *replayed[2], replayed[4])):
+            assert torch.equal(a, b)
+        assert eager[2].state[1] == 0
+        for s in (eager, replayed):                                     # the next batch goes behind this one
+            s[5].copy_(s[2].state[:1])
+            s[6].copy_(s[2].seq_lens)
 
 
 # ---- the run of them together ---------------------------------------------------------------------------------------
