@@ -5,11 +5,14 @@
 //   s_t = scale * ks * (q . kc_t),  out = sum_t softmax(s)_t vs vc_t,  lse = log sum_t exp s_t
 // with kc, vc the codes of token t and ks, vs the scales of its page and head.
 //
-// Both kernels multiply fp16: codes are whole numbers up to 127, exact in fp16, and so are a bf16 query's elements once its row
-// has been taken to a largest value between 1 and 2 by a power of two (an element under 2^-14 of that is off by 2^-25 at most).  The softmax runs in powers of two on
+// Codes are whole numbers up to 127, exact in fp16 and in bf16.  Scores of many rows are products of bf16, queries as they are; those of
+// few rows products of fp16, where a query's elements are exact too once its row has been taken to a largest value between 1 and 2 by a
+// power of two (an element under 2^-14 of that is off by 2^-25 at most).  Weights and values are fp16 in both.  The softmax runs in powers
+// of two on
 //   s'_t = s_t log2(e) + log2(vs),  p'_t = 2^(s'_t - m'),  m' about the largest s' so far,
 // so that the values' scale is inside the weight (p' is what fp16 has to hold, and it is largest where the products are) and the
-// products are with bare codes; the sum of the softmax is that of p'_t / vs = 2^(s_t - m').  A block of scale 0 holds zeros: any log2(vs) does for it.
+// products are with bare codes; the sum of the softmax is that of p'_t / vs = 2^(s_t - m').  A block of scale 0
+// holds zeros: any log2(vs) does for it.
 #pragma once
 #include "serve.cuh"
 

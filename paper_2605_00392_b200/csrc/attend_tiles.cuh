@@ -7,14 +7,18 @@
 //   O += P V    P from TMEM, V from shared memory, fp32 sums in TMEM
 // One CTA per SM takes items (two tiles) blockIdx.x, + gridDim.x, ...; what its warps do:
 //   0-3, 4-7  a row per thread of the first and second tile: softmax, output
-//   8-11      codes to bf16 (keys) and fp16 (values) in the swizzled operand layout (tiles of (token, 64 elements), K-major for the keys, MN-major for the values)
-//   12, 13    issue the MMAs of the first and second tile, in turns (one warp for both was the pace of the kernel)    14  bulk copies of codes    15  finds the items and fetches their queries, by TMA
+//   8-11      codes to bf16 (keys) and fp16 (values) in the swizzled operand layout (tiles of (token, 64 elements), K-major for the
+//             keys, MN-major for the values)
+//   12, 13    issue the MMAs of the first and second tile, in turns (one warp for both was the pace of the kernel)
+//   14        bulk copies of codes        15        finds the items and fetches their queries, by TMA
 // S of a tile's next block is issued behind the PV of this one, whose P it overwrites.  The tiles take turns: one's PV and S, then the
 // other's, so that one's softmax runs beside the other's MMAs (left to themselves they fell into step, both softmaxes, then
 // both MMAs: 4850 cycles a block).  One item's output leaves while the next one's scores are computed.
 // Everything large comes by bulk copies: with 227 KB of shared memory there are some 20 KB of L1 left, and ordinary loads of
 // 64 KB of queries, which need a line of it each while they are on their way, took 10,000 cycles.
-// A row's sums are rescaled only when its maximum has grown by more than 2^8 (the weights have that room in fp16).
+// A row's sums are rescaled only where 16 of its weights add up to more than 2^12 by the maximum so far: no weight has then left fp16's
+// range, and the sums, which are needed anyway, show it with less work than a maximum (772 us against 805 for 37 requests of 512 rows
+// that see 8512 tokens).
 // Bound by the tensor cores and, about as much, by the exponentials: 128 x 128 scores take 1024 cycles of either (16 exponentials a
 // cycle and SM; two products of 128^3 at 4096 multiply-adds).
 #pragma once
@@ -27,10 +31,11 @@ constexpr int kTlTiles = 2;
 constexpr int kTlBlock = 128;                        // tokens of a block
 constexpr int kTlSoft = kTlTiles * kTlRows;
 constexpr int kTlThreads = kTlSoft + 128 + 128;     // (the last warp only makes it 128 registers a thread)
-constexpr int kTlSoftRegs = 176, kTlCodeRegs = 56, kTlOtherRegs = 104;   // registers of a thread: 2, 1, 1 of four warpgroups
+constexpr int kTlSoftRegs = 200, kTlCodeRegs = 40, kTlOtherRegs = 72;    // registers of a thread: 2, 1, 1 of four warpgroups
 static_assert(2 * kTlSoftRegs + kTlCodeRegs + kTlOtherRegs <= 4 * 128, "what the block was launched with");
 constexpr int kTlGroups = kTlBlock / 16;             // a page holds at least 16 tokens: scales are per 16
 
+constexpr float kTlSlack = 4096.f;                   // what 16 weights may add up to (fp16 ends at 2^16)
 constexpr float kTlLarge = 1048576.f;                // scores under this are rounded by less than 2^-4
 
 template <int D> struct TlShape {
@@ -186,7 +191,7 @@ __device__ inline float max16(const float (&s)[16])
 }
 
 // The largest s' of 32 of a row's scores (two groups), and their weights p, the sum of these (without the values' scale) into l, the largest
-// s' - top into `most`.  The scores come from TMEM 32 at a time: a thread that keeps its 128 spills whatever else it has, and what is
+// sum of 16 into `most`.  The scores come from TMEM 32 at a time: a thread that keeps its 128 spills whatever else it has, and what is
 // spilled comes back from L2 (shared memory has left L1 next to nothing).
 __device__ inline float tile_top(const uint32_t (&v)[32], const float4 *group, float factor, float now)
 {
@@ -212,7 +217,6 @@ __device__ inline void tile_weights(const uint32_t (&v)[32], const float4 *group
 #pragma unroll
         for (int e = 0; e < 16; e += 2)
             unpack2(fma2(pack2(__uint_as_float(v[16 * h + e]), __uint_as_float(v[16 * h + e + 1])), k2, b2), w[e], w[e + 1]);
-        most = fmaxf(most, max16(w));
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
             w[e] = ex2(w[e]);
@@ -222,7 +226,9 @@ __device__ inline void tile_weights(const uint32_t (&v)[32], const float4 *group
         }
         float s0, s1;
         unpack2(sum2, s0, s1);
-        l = fmaf(s0 + s1, g.z, l);
+        s0 += s1;
+        most = fmaxf(most, s0);
+        l = fmaf(s0, g.z, l);
     }
 }
 // The same where tokens from `left` on are not seen, or scores are so large that their own rounding matters: it is what the maximum
@@ -331,191 +337,191 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
 
     // (registers: one instruction for each warpgroup, ahead of all that the warpgroup does)
     if (warp >= 12) {
-    regs_fewer<kTlOtherRegs>();
-    if (warp == 15) {
-        // ---------------- the work: items blockIdx.x, + gridDim.x, ... that have rows; their queries, as they are, in the operand's
-        // layout already
-        const int per = a.batch * a.c.kv_heads, all = row_blocks * per;
-        auto number = [&](int round) { return round * (int)gridDim.x + (int)(round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x); };
-        const int rounds = (all + (int)gridDim.x - 1) / (int)gridDim.x;
-        int at = 0;
-        bool ok = true;
-        uint32_t uses[kTlTiles] = {0, 0};
-#pragma unroll 1
-        for (uint32_t k = 0; ok; ++k) {
-            TlItem t;
-            t.i = -1;
-            // 32 of the numbers at a time, one per lane (bounds that are far above the requests' lengths leave most of them empty)
-#pragma unroll 1
-            for (; at < rounds; at += 32) {
-                const int mine = number(at + lane);
-                bool has = false;
-                if (at + lane < rounds && mine < all) {
-                    // the last rows of every request first: with a causal mask they have the most to do
-                    const int rest = mine % per;
-                    t.i = rest / a.c.kv_heads;
-                    t.head = rest - t.i * a.c.kv_heads;
-                    t.j0 = (row_blocks - 1 - mine / per) * kTlTiles * tile_tokens;
-                    has = attend_request(a, t.i, t.row0, t.n, t.len) && t.j0 < t.n;
-                }
-                const uint32_t found = __ballot_sync(0xffffffffu, has);
-                if (found) {
-                    const int from = __ffs(found) - 1;
-                    at += from + 1;
-                    t.i = __shfl_sync(0xffffffffu, t.i, from);
-                    t.head = __shfl_sync(0xffffffffu, t.head, from);
-                    t.j0 = __shfl_sync(0xffffffffu, t.j0, from);
-                    t.row0 = __shfl_sync(0xffffffffu, t.row0, from);
-                    t.n = __shfl_sync(0xffffffffu, t.n, from);
-                    t.len = __shfl_sync(0xffffffffu, t.len, from);
-#pragma unroll
-                    for (int x = 0; x < kTlTiles; ++x) {
-                        const int first = t.j0 + x * tile_tokens, last = min(first + tile_tokens, t.n) - 1;
-                        const int end = first >= t.n || t.len < 0 ? 0 : a.causal ? t.len - t.n + 1 + last : t.len;
-                        t.blocks[x] = (max(end, 0) + kTlBlock - 1) / kTlBlock;
-                    }
-                    break;
-                }
+        regs_fewer<kTlOtherRegs>();
+        if (warp == 15) {
+            // ---------------- the work: items blockIdx.x, + gridDim.x, ... that have rows; their queries, as they are, in the operand's
+            // layout already
+            const int per = a.batch * a.c.kv_heads, all = row_blocks * per;
+            auto number = [&](int round) { return round * (int)gridDim.x + (int)(round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x); };
+            const int rounds = (all + (int)gridDim.x - 1) / (int)gridDim.x;
+            int at = 0;
+            bool ok = true;
+            uint32_t uses[kTlTiles] = {0, 0};
+    #pragma unroll 1
+            for (uint32_t k = 0; ok; ++k) {
+                TlItem t;
                 t.i = -1;
-            }
-            if (k >= kTlItems) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&sh->item_empty[k % kTlItems], (k / kTlItems - 1) & 1));
-            if (ok && lane == 0) {
-                sh->item[k % kTlItems] = t;
-                ptx::mbar_arrive(&sh->item_full[k % kTlItems]);
-            }
-            if (t.i < 0) break;
-#pragma unroll
-            for (int x = 0; x < kTlTiles; ++x) {
-                if (!ok || t.blocks[x] == 0) continue;
-                if (uses[x] > 0) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&sh->q_empty[x], (uses[x] - 1) & 1));
-                if (ok && lane == 0) {
-                    ptx::mbar_arrive_expect_tx(&sh->q_full[x], (uint32_t)(S::kSlabs * tile_tokens * a.group * 128));
-                    for (int b = 0; b < S::kSlabs; ++b)
-                        ptx::tma_load_3d(s_u32 + x * S::kOperand + b * S::kSlab, &map_q, &sh->q_full[x], b * 64, t.head * a.group,
-                                         t.row0 + t.j0 + x * tile_tokens);
-                }
-                __syncwarp();
-                if (ok) ++uses[x];
-            }
-        }
-        if (!ok) sh->gave_up = 1;
-        // no copy is left on its way into memory that this CTA gives back
-#pragma unroll
-        for (int x = 0; x < kTlTiles; ++x)
-            if (uses[x] > 0) ptx::mbar_wait(&sh->q_full[x], (uses[x] - 1) & 1);
-    } else if (warp == 14) {
-        // ---------------- codes of the items' blocks, and their scales ----------------------------------------
-        const int per_page = min(a.c.page_size, kTlBlock), copies = kTlBlock / per_page;   // a page of a head is one piece of memory
-        TlItem t;
-        bool ok = true;
-        uint32_t n = 0, copy = 0;                    // blocks, slots so far
-#pragma unroll 1
-        for (uint32_t item = 0; ok && (ok = tl_take(sh, item, t)) && t.i >= 0; ++item) {
-            const int most = max(t.blocks[0], t.blocks[1]);
-#pragma unroll 1
-            for (int j = 0; ok && j < most; ++j, ++n) {
-                // lane: a copy's page, and (lane < 8) the page of its 16 tokens.  Tokens behind the end are not fetched: what lies in
-                // the slot are codes too, and nobody sees them
-                const int t0 = j * kTlBlock, t_copy = t0 + lane * per_page, t_group = t0 + lane * 16;
-                const int page = lane < copies && t_copy < t.len ? attend_page(a, t.i, t_copy) : -1;
-                const int page_g = lane < kTlGroups && t_group < t.len ? attend_page(a, t.i, t_group) : -1;
-                if (lane < kTlGroups) {
-                    const int64_t block = (int64_t)max(page_g, 0) * a.c.kv_heads + t.head;
-                    const float nan = __uint_as_float(0x7fc00000u);
-                    float lv, inv;
-                    value_scale(page_g < 0 ? nan : __ldg(a.c.v_scale + block), lv, inv);
-                    sh->group[n % kTlGroupRing][lane] = make_float4(page_g < 0 ? nan : __ldg(a.c.k_scale + block), lv, inv, 0.f);
-                }
-                const uint32_t bytes = (uint32_t)(__popc(__ballot_sync(0xffffffffu, page >= 0)) * per_page * D);
-                const int64_t from = ((int64_t)max(page, 0) * a.c.kv_heads + t.head) * a.c.page_size * D;
-#pragma unroll 1
-                for (int v = 0; ok && v < 2; ++v, ++copy) {
-                    const uint32_t slot = copy % S::kSlots, turn = copy / S::kSlots;
-                    if (turn > 0) ok = ptx::mbar_wait(&sh->code_empty[slot], (turn - 1) & 1);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    if (lane == 0) ptx::mbar_arrive_expect_tx(&sh->code_full[slot], bytes);
-                    __syncwarp();
-                    if (page >= 0)
-                        ptx::bulk_load(code_u32 + slot * S::kSlot + lane * per_page * D, (v ? a.c.v : a.c.k) + from, (uint32_t)(per_page * D), &sh->code_full[slot]);
-                }
-            }
-        }
-        if (!ok) sh->gave_up = 1;
-        // no copy is left on its way into memory that this CTA gives back
-        for (uint32_t c = copy > S::kSlots ? copy - S::kSlots : 0; c < copy; ++c)
-            ptx::mbar_wait(&sh->code_full[c % S::kSlots], c / S::kSlots & 1);
-    } else {
-        // ---------------- the MMAs of tile x ----------------------------------------------------------------
-        // the whole warp walks the blocks, one elected lane issues
-        const int x = warp - 12;
-        const bool issuer = elect_one();
-        const uint32_t id_s = ptx::idesc_bf16(kTlRows, kTlBlock, false, false), id_o = idesc_f16(kTlRows, D, true);
-        const uint32_t t_s = tmem + x * 128, t_o = tmem + 256 + x * D;
-        // descriptors differ from these by multiples of 16 bytes in the address (their low 14 bits, which never carry)
-        const uint64_t d_q = ptx::smem_desc_sw128(s_u32 + x * S::kOperand, 16, 1024), d_k = ptx::smem_desc_sw128(k_u32, 16, 1024);
-        const uint64_t d_v = ptx::smem_desc_sw128(v_u32, S::kSlab, 1024);
-        bool ok = true;
-        uint32_t n = 0, step = 0, items = 0, turns = 0;      // blocks and steps; this tile's items and blocks so far
-        TlItem t;
-#pragma unroll 1
-        for (uint32_t item = 0; ok && (ok = tl_take(sh, item, t)) && t.i >= 0; ++item) {
-            const int most = max(t.blocks[0], t.blocks[1]), mine = x ? t.blocks[1] : t.blocks[0];
-            // step j: products of block j - 1, scores of block j; n is block j's number.  A block that this tile sees nothing of is passed on
-            // once it is there (not before: its buffer's turns would be mixed up)
-#pragma unroll 1
-            for (int j = 0; j <= most && most > 0; ++j, ++n, ++step) {
-                const uint32_t s = n & 1, s_before = s ^ 1;
-                const bool products = j > 0 && j <= mine, scores = j < mine;
-                // what is there early is waited for first, the weights last: their way to the next scores is the kernel's longest
-                if (j > 0) ok = ptx::mbar_wait(&sh->v_full[s_before], ((n - 1) >> 1) & 1);
-                if (j < most) ok = ok && ptx::mbar_wait(&sh->k_full[s], (n >> 1) & 1);
-                if (j == 0 && mine > 0) ok = ok && ptx::mbar_wait(&sh->q_full[x], items & 1);
-                if (j == 1 && mine > 0 && items > 0) ok = ok && ptx::mbar_wait(&sh->o_empty[x], (items - 1) & 1);   // (the last item's output is out of TMEM)
-                // the other tile's turn before this
-                if (x > 0 || step > 0) ok = ok && ptx::mbar_wait(&sh->turn[x ^ 1], (x ? step : step - 1) & 1);
-                if (products) {
-                    ok = ok && ptx::mbar_wait(&sh->p_full[x], turns & 1);
-                    ++turns;
-                }
-                if (!ok) break;
-                ptx::tc_fence_after();
-                if (products && issuer) {
-                    const uint64_t v0 = d_v + s_before * (S::kOperand >> 4);
-#pragma unroll
-                    for (int k = 0; k < kTlBlock / 16; ++k) umma_f16_ts(t_o, t_s + k * 8, v0 + k * (2048 >> 4), id_o, j - 1 + k > 0);
-                    ptx::umma_commit(&sh->v_empty[s_before]);
-                    if (j == mine) ptx::umma_commit(&sh->o_full[x]);
-                } else if (j > 0 && issuer) {
-                    ptx::mbar_arrive(&sh->v_empty[s_before]);
-                }
-                if (j < most) {
-                    if (scores && issuer) {
-                        const uint64_t k0 = d_k + s * (S::kOperand >> 4);
-#pragma unroll
-                        for (int k = 0; k < D / 16; ++k) {
-                            const int at = ((k >> 2) * S::kSlab + (k & 3) * 32) >> 4;
-                            ptx::umma_bf16(t_s, d_q + at, k0 + at, id_s, k > 0);
+                // 32 of the numbers at a time, one per lane (bounds that are far above the requests' lengths leave most of them empty)
+    #pragma unroll 1
+                for (; at < rounds; at += 32) {
+                    const int mine = number(at + lane);
+                    bool has = false;
+                    if (at + lane < rounds && mine < all) {
+                        // the last rows of every request first: with a causal mask they have the most to do
+                        const int rest = mine % per;
+                        t.i = rest / a.c.kv_heads;
+                        t.head = rest - t.i * a.c.kv_heads;
+                        t.j0 = (row_blocks - 1 - mine / per) * kTlTiles * tile_tokens;
+                        has = attend_request(a, t.i, t.row0, t.n, t.len) && t.j0 < t.n;
+                    }
+                    const uint32_t found = __ballot_sync(0xffffffffu, has);
+                    if (found) {
+                        const int from = __ffs(found) - 1;
+                        at += from + 1;
+                        t.i = __shfl_sync(0xffffffffu, t.i, from);
+                        t.head = __shfl_sync(0xffffffffu, t.head, from);
+                        t.j0 = __shfl_sync(0xffffffffu, t.j0, from);
+                        t.row0 = __shfl_sync(0xffffffffu, t.row0, from);
+                        t.n = __shfl_sync(0xffffffffu, t.n, from);
+                        t.len = __shfl_sync(0xffffffffu, t.len, from);
+    #pragma unroll
+                        for (int x = 0; x < kTlTiles; ++x) {
+                            const int first = t.j0 + x * tile_tokens, last = min(first + tile_tokens, t.n) - 1;
+                            const int end = first >= t.n || t.len < 0 ? 0 : a.causal ? t.len - t.n + 1 + last : t.len;
+                            t.blocks[x] = (max(end, 0) + kTlBlock - 1) / kTlBlock;
                         }
-                        ptx::umma_commit(&sh->s_full[x]);
-                        ptx::umma_commit(&sh->k_empty[s]);
-                        if (j + 1 == mine) ptx::umma_commit(&sh->q_empty[x]);
-                    } else if (issuer) {
-                        ptx::mbar_arrive(&sh->k_empty[s]);
+                        break;
+                    }
+                    t.i = -1;
+                }
+                if (k >= kTlItems) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&sh->item_empty[k % kTlItems], (k / kTlItems - 1) & 1));
+                if (ok && lane == 0) {
+                    sh->item[k % kTlItems] = t;
+                    ptx::mbar_arrive(&sh->item_full[k % kTlItems]);
+                }
+                if (t.i < 0) break;
+    #pragma unroll
+                for (int x = 0; x < kTlTiles; ++x) {
+                    if (!ok || t.blocks[x] == 0) continue;
+                    if (uses[x] > 0) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&sh->q_empty[x], (uses[x] - 1) & 1));
+                    if (ok && lane == 0) {
+                        ptx::mbar_arrive_expect_tx(&sh->q_full[x], (uint32_t)(S::kSlabs * tile_tokens * a.group * 128));
+                        for (int b = 0; b < S::kSlabs; ++b)
+                            ptx::tma_load_3d(s_u32 + x * S::kOperand + b * S::kSlab, &map_q, &sh->q_full[x], b * 64, t.head * a.group,
+                                             t.row0 + t.j0 + x * tile_tokens);
+                    }
+                    __syncwarp();
+                    if (ok) ++uses[x];
+                }
+            }
+            if (!ok) sh->gave_up = 1;
+            // no copy is left on its way into memory that this CTA gives back
+    #pragma unroll
+            for (int x = 0; x < kTlTiles; ++x)
+                if (uses[x] > 0) ptx::mbar_wait(&sh->q_full[x], (uses[x] - 1) & 1);
+        } else if (warp == 14) {
+            // ---------------- codes of the items' blocks, and their scales ----------------------------------------
+            const int per_page = min(a.c.page_size, kTlBlock), copies = kTlBlock / per_page;   // a page of a head is one piece of memory
+            TlItem t;
+            bool ok = true;
+            uint32_t n = 0, copy = 0;                    // blocks, slots so far
+    #pragma unroll 1
+            for (uint32_t item = 0; ok && (ok = tl_take(sh, item, t)) && t.i >= 0; ++item) {
+                const int most = max(t.blocks[0], t.blocks[1]);
+    #pragma unroll 1
+                for (int j = 0; ok && j < most; ++j, ++n) {
+                    // lane: a copy's page, and (lane < 8) the page of its 16 tokens.  Tokens behind the end are not fetched: what lies in
+                    // the slot are codes too, and nobody sees them
+                    const int t0 = j * kTlBlock, t_copy = t0 + lane * per_page, t_group = t0 + lane * 16;
+                    const int page = lane < copies && t_copy < t.len ? attend_page(a, t.i, t_copy) : -1;
+                    const int page_g = lane < kTlGroups && t_group < t.len ? attend_page(a, t.i, t_group) : -1;
+                    if (lane < kTlGroups) {
+                        const int64_t block = (int64_t)max(page_g, 0) * a.c.kv_heads + t.head;
+                        const float nan = __uint_as_float(0x7fc00000u);
+                        float lv, inv;
+                        value_scale(page_g < 0 ? nan : __ldg(a.c.v_scale + block), lv, inv);
+                        sh->group[n % kTlGroupRing][lane] = make_float4(page_g < 0 ? nan : __ldg(a.c.k_scale + block), lv, inv, 0.f);
+                    }
+                    const uint32_t bytes = (uint32_t)(__popc(__ballot_sync(0xffffffffu, page >= 0)) * per_page * D);
+                    const int64_t from = ((int64_t)max(page, 0) * a.c.kv_heads + t.head) * a.c.page_size * D;
+    #pragma unroll 1
+                    for (int v = 0; ok && v < 2; ++v, ++copy) {
+                        const uint32_t slot = copy % S::kSlots, turn = copy / S::kSlots;
+                        if (turn > 0) ok = ptx::mbar_wait(&sh->code_empty[slot], (turn - 1) & 1);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        if (lane == 0) ptx::mbar_arrive_expect_tx(&sh->code_full[slot], bytes);
+                        __syncwarp();
+                        if (page >= 0)
+                            ptx::bulk_load(code_u32 + slot * S::kSlot + lane * per_page * D, (v ? a.c.v : a.c.k) + from, (uint32_t)(per_page * D), &sh->code_full[slot]);
                     }
                 }
-                if (issuer) ptx::mbar_arrive(&sh->turn[x]);
-                __syncwarp();
             }
-            if (most > 0) --n;                       // (the next item's first block has the number of the step without scores)
-            items += mine > 0;
+            if (!ok) sh->gave_up = 1;
+            // no copy is left on its way into memory that this CTA gives back
+            for (uint32_t c = copy > S::kSlots ? copy - S::kSlots : 0; c < copy; ++c)
+                ptx::mbar_wait(&sh->code_full[c % S::kSlots], c / S::kSlots & 1);
+        } else {
+            // ---------------- the MMAs of tile x ----------------------------------------------------------------
+            // the whole warp walks the blocks, one elected lane issues
+            const int x = warp - 12;
+            const bool issuer = elect_one();
+            const uint32_t id_s = ptx::idesc_bf16(kTlRows, kTlBlock, false, false), id_o = idesc_f16(kTlRows, D, true);
+            const uint32_t t_s = tmem + x * 128, t_o = tmem + 256 + x * D;
+            // descriptors differ from these by multiples of 16 bytes in the address (their low 14 bits, which never carry)
+            const uint64_t d_q = ptx::smem_desc_sw128(s_u32 + x * S::kOperand, 16, 1024), d_k = ptx::smem_desc_sw128(k_u32, 16, 1024);
+            const uint64_t d_v = ptx::smem_desc_sw128(v_u32, S::kSlab, 1024);
+            bool ok = true;
+            uint32_t n = 0, step = 0, items = 0, turns = 0;      // blocks and steps; this tile's items and blocks so far
+            TlItem t;
+    #pragma unroll 1
+            for (uint32_t item = 0; ok && (ok = tl_take(sh, item, t)) && t.i >= 0; ++item) {
+                const int most = max(t.blocks[0], t.blocks[1]), mine = x ? t.blocks[1] : t.blocks[0];
+                // step j: products of block j - 1, scores of block j; n is block j's number.  A block that this tile sees nothing of is passed on
+                // once it is there (not before: its buffer's turns would be mixed up)
+    #pragma unroll 1
+                for (int j = 0; j <= most && most > 0; ++j, ++n, ++step) {
+                    const uint32_t s = n & 1, s_before = s ^ 1;
+                    const bool products = j > 0 && j <= mine, scores = j < mine;
+                    // what is there early is waited for first, the weights last: their way to the next scores is the kernel's longest
+                    if (j > 0) ok = ptx::mbar_wait(&sh->v_full[s_before], ((n - 1) >> 1) & 1);
+                    if (j < most) ok = ok && ptx::mbar_wait(&sh->k_full[s], (n >> 1) & 1);
+                    if (j == 0 && mine > 0) ok = ok && ptx::mbar_wait(&sh->q_full[x], items & 1);
+                    if (j == 1 && mine > 0 && items > 0) ok = ok && ptx::mbar_wait(&sh->o_empty[x], (items - 1) & 1);   // (the last item's output is out of TMEM)
+                    // the other tile's turn before this
+                    if (x > 0 || step > 0) ok = ok && ptx::mbar_wait(&sh->turn[x ^ 1], (x ? step : step - 1) & 1);
+                    if (products) {
+                        ok = ok && ptx::mbar_wait(&sh->p_full[x], turns & 1);
+                        ++turns;
+                    }
+                    if (!ok) break;
+                    ptx::tc_fence_after();
+                    if (products && issuer) {
+                        const uint64_t v0 = d_v + s_before * (S::kOperand >> 4);
+    #pragma unroll
+                        for (int k = 0; k < kTlBlock / 16; ++k) umma_f16_ts(t_o, t_s + k * 8, v0 + k * (2048 >> 4), id_o, j - 1 + k > 0);
+                        ptx::umma_commit(&sh->v_empty[s_before]);
+                        if (j == mine) ptx::umma_commit(&sh->o_full[x]);
+                    } else if (j > 0 && issuer) {
+                        ptx::mbar_arrive(&sh->v_empty[s_before]);
+                    }
+                    if (j < most) {
+                        if (scores && issuer) {
+                            const uint64_t k0 = d_k + s * (S::kOperand >> 4);
+    #pragma unroll
+                            for (int k = 0; k < D / 16; ++k) {
+                                const int at = ((k >> 2) * S::kSlab + (k & 3) * 32) >> 4;
+                                ptx::umma_bf16(t_s, d_q + at, k0 + at, id_s, k > 0);
+                            }
+                            ptx::umma_commit(&sh->s_full[x]);
+                            ptx::umma_commit(&sh->k_empty[s]);
+                            if (j + 1 == mine) ptx::umma_commit(&sh->q_empty[x]);
+                        } else if (issuer) {
+                            ptx::mbar_arrive(&sh->k_empty[s]);
+                        }
+                    }
+                    if (issuer) ptx::mbar_arrive(&sh->turn[x]);
+                    __syncwarp();
+                }
+                if (most > 0) --n;                       // (the next item's first block has the number of the step without scores)
+                items += mine > 0;
+            }
+            if (!ok) sh->gave_up = 1;
+            // all MMAs done (also after a wait that gave up: the memory they use is about to be freed)
+            if (issuer) ptx::umma_commit(&sh->done);
+            __syncwarp();
+            if (!ptx::mbar_wait(&sh->done, 0)) sh->gave_up = 1;
         }
-        if (!ok) sh->gave_up = 1;
-        // all MMAs done (also after a wait that gave up: the memory they use is about to be freed)
-        if (issuer) ptx::umma_commit(&sh->done);
-        __syncwarp();
-        if (!ptx::mbar_wait(&sh->done, 0)) sh->gave_up = 1;
-    }
     } else if (warp >= 8) {
         regs_fewer<kTlCodeRegs>();
         // ---------------- codes to bf16 and fp16 ---------------------------------------------------------------------
@@ -560,7 +566,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
 #pragma unroll 1
         for (uint32_t item = 0;; ++item) {
             float top = kAtNothing, l = 0.f;
-            const int warp_most = __shfl_sync(0xffffffffu, end, 31); const int warp_end = __shfl_sync(0xffffffffu, end, 0);      // the first row of the warp sees the fewest tokens
+            const int warp_most = __shfl_sync(0xffffffffu, end, 31), warp_end = __shfl_sync(0xffffffffu, end, 0);   // (the first row sees the fewest tokens)
 #pragma unroll 1
             for (int j = 0; ok && j < blocks; ++j, ++turns) {
                 if (!(ok = ptx::mbar_wait(&sh->s_full[x], turns & 1))) break;
@@ -609,7 +615,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                         break;
                     }
                     uint32_t va[32], vb[32], p[64];
-                    float most = -INFINITY, more = 0.f;
+                    float most = 0.f, more = 0.f;
                     ptx::tmem_ld32(t_s, va);
                     ptx::tmem_ld_wait();
                     ptx::tmem_ld32(t_s + 32, vb);
@@ -622,7 +628,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                     tile_weights(va, group + 4, factor, top, p + 32, most, more);
                     ptx::tmem_ld_wait();
                     tile_weights(vb, group + 6, factor, top, p + 48, most, more);
-                    if (!first && __any_sync(0xffffffffu, most > kAtSlack)) continue;
+                    if (!first && __any_sync(0xffffffffu, most > kTlSlack)) continue;
                     l += more;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_st16(t_s + 16 * c, *reinterpret_cast<uint32_t (*)[16]>(p + 16 * c));
