@@ -294,6 +294,101 @@ def large_n_line(args) -> dict:
             "shapes": shapes}
 
 
+def run_answer(args) -> None:
+    """`--step answer`: from the pruned batch to the answer's tokens, one layer of 10 heads of 128: the pruning run, page
+    tables, norms and rotation, the 8-bit cache write and attention over the cache, for the whole batch (prefill) and for a token
+    of each request (decode).  One GPU; one JSON line."""
+    print(json.dumps(answer_line(args)), flush=True)
+
+
+def answer_line(args) -> dict:
+    if not torch.cuda.is_available():
+        raise SystemExit("bench.py needs a CUDA device: the pruning path has no CPU fallback")
+    from paper_2605_00392_b200 import binding, synth
+    dev = torch.device("cuda", 0)
+    torch.cuda.set_device(dev)
+    steps, warm = max(1, min(args.steps, 50)), max(args.warmup, 3)
+    heads, dim, page = 10, 128, 64
+    w = synth.make(WORKLOAD)
+    batch, rows, longest = w.batch, w.total_tokens, w.max_tokens
+    plan = binding.Plan(w.d, w.X.dtype, batch, rows, longest, device=dev)
+    fields = {k: (int(v) if k in ("dynamic", "iters") else float(v)) for k, v in w.params.items()}
+    params = binding.make_params(torch.from_numpy(w.rho).to(dev), **fields)
+    X, offs, out = w.X.to(dev), torch.from_numpy(w.offsets).to(dev), binding.Outputs.allocate(rows, batch, w.d, w.X.dtype, dev)
+    pages = -(-(longest + 1) // page)
+    cache = binding.PagedCache.allocate(batch * pages, heads, page, dim, dev)
+    tables = torch.full((batch, pages), -1, dtype=torch.int32, device=dev)
+    free, head = torch.randperm(batch * pages, device=dev).int(), torch.zeros(1, dtype=torch.int32, device=dev)
+    freq = binding.rope_frequencies(dim, 1e4, dev)
+    weight = torch.ones(dim, dtype=torch.bfloat16, device=dev)
+
+    def leg(n, offsets, context, index, max_q):
+        states = torch.randn(n, 3 * heads * dim, device=dev).to(torch.bfloat16)          # a fused projection's rows
+        q, k, v = (t.view(n, heads, dim) for t in states.split(heads * dim, 1))
+        m = binding.PageMap.allocate(n, batch, dev)
+        o = torch.zeros(n, heads, dim, dtype=torch.bfloat16, device=dev)
+        ws = torch.empty(binding.cache_attend_workspace(batch, max_q, pages * page, heads, heads, dim), dtype=torch.uint8, device=dev)
+        return m, {
+            "page_map": lambda: binding.map_pages(offsets, tables, free, head, m, page_size=page, context_lens=context, token_index=index),
+            "qk_norm_rope": lambda: binding.qk_norm_rope(q, k, m.positions, freq, weight, weight),
+            "cache_write": lambda: binding.cache_write(k, v, m.slot_map, cache),
+            "cache_attend": lambda: binding.cache_attend(q, offsets, m.seq_lens, tables, cache, max_q_len=max_q,
+                                                         max_seq_len=pages * page, out=o, workspace=ws)}
+
+    prefill, calls = leg(rows, out.out_offsets, None, out.kept_idx, longest)
+    calls = {"prune": lambda: plan.run(X, offs, params, out), **calls}
+    for call in calls.values():
+        call()
+    torch.cuda.synchronize()
+    assert plan.query_status() == 0 and prefill.state[1] == 0
+    lens = prefill.seq_lens.clone()
+    steps_of = torch.arange(batch + 1, dtype=torch.int32, device=dev)
+    token, decode = leg(batch, steps_of, lens, None, 1)
+    flush = torch.empty(160 << 20, dtype=torch.uint8, device=dev)      # larger than L2
+
+    def time_leg(calls):
+        ms = {name: 0.0 for name in calls}
+        for t in range(warm + steps):
+            flush.zero_()                                              # no step finds its input in L2
+            marks = [torch.cuda.Event(enable_timing=True) for _ in range(len(calls) + 1)]
+            marks[0].record()
+            for mark, call in zip(marks[1:], calls.values()):
+                call()
+                mark.record()
+            torch.cuda.synchronize()
+            if t >= warm:
+                for name, a, b in zip(calls, marks, marks[1:]):
+                    ms[name] += a.elapsed_time(b) / steps
+        return ms
+
+    first = time_leg(calls)
+    head.copy_(prefill.state[:1])                                      # the decode step's pages come behind the prefill's
+    per_token = time_leg(decode)
+    assert token.state[1] == 0 and plan.query_status() == 0
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        for call in decode.values():
+            call()
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    for _ in range(warm):
+        g.replay()
+    e0.record()
+    for _ in range(steps):
+        g.replay()
+    e1.record()
+    torch.cuda.synchronize()
+    kept = int(lens.sum())
+    launches = plan.last_launch_count + 4
+    plan.close()
+    return {"metric": "tokens of pruned images into the cache/sec", "value": kept / (sum(first.values()) / 1e3), "unit": "tokens/s",
+            "n_gpus": 1, "steps": steps, "warmup": warm, "ms_per_step": sum(first.values()), "higher_is_better": True,
+            "dtype": "bf16, int8 cache", "data": "synthetic",
+            "timing": "CUDA events around each call, L2 flushed between steps; the decode step also as a captured graph, back to back",
+            "config": {"workload": WORKLOAD_DESC, "layers": 1, "heads": heads, "head_dim": dim, "page_size": page},
+            "prefill_ms": first, "decode_ms": per_token, "decode_graph_ms": e0.elapsed_time(e1) / steps, "decode_requests": batch,
+            "gpu_launches": launches * steps}
+
+
 def sweep_line(w0, steps: int, warm: int) -> dict:
     """1024 images x 400 tokens (the Large batch tiled 16 times on the device: 1.05 GB of tokens, far beyond L2):
     the batch on which the path's HBM bound can be approached.  One GPU."""
@@ -384,9 +479,10 @@ def self_launch(args) -> None:
 
 def main() -> None:
     ap = argparse.ArgumentParser()
-    ap.add_argument("--step", default="prune", choices=["prune", "density", "largen"],
+    ap.add_argument("--step", default="prune", choices=["prune", "density", "largen", "answer"],
                     help="prune: the pruning path (the headline); density: the textual-density kernel alone; "
-                         "largen: the pruning path on images of 2137 and 4512 tokens")
+                         "largen: the pruning path on images of 2137 and 4512 tokens; answer: from the pruned batch through the "
+                         "8-bit cache and attention to a token of each request")
     ap.add_argument("--gpus", type=int, default=1)
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--warmup", type=int, default=10)
@@ -416,6 +512,10 @@ def main() -> None:
     if args.step == "largen":
         if rank == 0:
             run_large_n(args)
+        return
+    if args.step == "answer":
+        if rank == 0:
+            run_answer(args)
         return
 
     if not torch.cuda.is_available():
