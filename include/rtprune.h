@@ -418,7 +418,7 @@ rtprune_status_t rtprune_cache_write(void *cuda_stream, rtprune_dtype_t dtype, c
  *                grid (and so how sums are put together), not what is computed
  *   block_tables DEVICE int32 [batch] rows, table_stride apart, of max_pages entries
  *   out          DEVICE bf16 [rows][q_heads][head_dim], 32-byte aligned; lse DEVICE float [rows][q_heads], may be NULL.
- *                Rows of no request are left as they are.
+ *                Rows of no request are left as they are.  Neither may overlap what is read.
  *   workspace    DEVICE, 256-byte aligned, of what rtprune_cache_attend_workspace says for the same sizes; its contents do not
  *                matter and it serves one call at a time
  * q_heads a multiple of kv_heads, at most 4096.

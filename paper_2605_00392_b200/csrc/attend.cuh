@@ -45,7 +45,7 @@ __device__ inline bool attend_request(const AttendArgs &a, int i, int &row0, int
     n = hi - row0;
     len = __ldg(a.seq_lens + i);
     if (len < 0 || len > a.max_len) len = -1;
-    return row0 >= 0 && n > 0 && hi <= a.rows && n <= a.max_q_len;
+    return row0 >= 0 && hi > row0 && hi <= a.rows && n <= a.max_q_len;
 }
 
 // The page of token t, or -1.

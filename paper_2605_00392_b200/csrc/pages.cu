@@ -341,7 +341,7 @@ extern "C" rtprune_status_t rtprune_page_map(void *cuda_stream, const int32_t *o
     while ((1 << shift) < page_size) ++shift;
     const int64_t per_cta = kPmThreads * kPmRows;
     const size_t smem = (size_t)(2 * batch + 1) * 4;
-    if (smem > 48 * 1024) {
+    if (smem > 40 * 1024) {                  // (the kernel's own few bytes count towards the 48 KB too)
         if (cudaFuncSetAttribute(page_map_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (2 * kPmMaxBatch + 1) * 4) != cudaSuccess)
             return RTPRUNE_ERR_CUDA;
     }
@@ -367,7 +367,7 @@ extern "C" rtprune_status_t rtprune_cache_write(void *cuda_stream, rtprune_dtype
     if (!k || !v || !slot_map || k_stride < width || v_stride < width || k_stride % vec || v_stride % vec ||
         ((uintptr_t)k | (uintptr_t)v) & 15u)
         return RTPRUNE_ERR_INVALID_ARG;
-    if (rows > INT32_MAX - kCwMaxWindow) return RTPRUNE_ERR_UNSUPPORTED;
+    if (rows > INT32_MAX - 4 * kCwMaxWindow) return RTPRUNE_ERR_UNSUPPORTED;     // (a CTA looks a window and a page ahead)
     const int sms = device_sms();
     if (!sms) return RTPRUNE_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -58,6 +58,18 @@ def test_page_map(page, new, ctx, pad, indexed):
     assert out.state.tolist() == [want[4], 0] and (wide[:, most:] == -9).all()
 
 
+@pytest.mark.parametrize("batch", [5000, 6135, 6140, 6143, 6144, 16384])
+def test_page_map_large_batches(batch):
+    new = [i % 3 for i in range(batch)]
+    off, tables = np.concatenate([[0], np.cumsum(new)]), np.full((batch, 1), -1)
+    free = np.arange(batch, dtype=np.int32)[::-1].copy()
+    want = ref.page_map(off, [0] * batch, sum(new), 16, free, 0, tables)
+    t, out = _i32(np.full((batch, 1), -1)), binding.PageMap.allocate(sum(new), batch, DEV)
+    binding.map_pages(_i32(off), t, _i32(free), _i32([0]), out, page_size=16)
+    for got, w in zip((t, out.slot_map, out.positions, out.seq_lens), want):
+        np.testing.assert_array_equal(got.cpu().numpy(), w)
+
+
 def test_page_map_without_contexts_and_with_bases_alone():
     out = binding.PageMap.allocate(6, 2, DEV)
     t = torch.full((2, 2), -1, dtype=torch.int32, device=DEV)
@@ -506,6 +518,18 @@ def test_page_map_rope_and_write_in_a_graph_on_another_stream():
         for s in (eager, replayed):                                     # the next batch goes behind this one
             s[5].copy_(s[2].state[:1])
             s[6].copy_(s[2].seq_lens)
+
+
+@pytest.mark.parametrize("low,high", [(2 ** 31 - 1, -5), (5, 2), (-3, 2), (2, 2 ** 31 - 1), (-2 ** 31, 2 ** 31 - 1)])
+def test_attend_offsets_outside_the_contract(low, high):
+    # the request between two sound ones has offsets that are none: passed over, whatever the bounds allow
+    q, off, L, tables, cache = _batch([2, 1, 2], [9, 9, 9], 4, 2, 64, 16, 3)
+    clean = binding.cache_attend(q, off, L, tables, cache, max_q_len=2, max_seq_len=16)
+    for max_q in (2, 2 ** 30, 2 ** 31 - 1):
+        o = _i32([0, 2, low, high])
+        got = binding.cache_attend(q, o, L, tables, cache, max_q_len=max_q, max_seq_len=16, out=torch.full_like(q, 3.0))
+        torch.testing.assert_close(got[:2], clean[:2], rtol=2 ** -6, atol=1e-3)
+        assert (got[5:] == 3).all()
 
 
 # ---- the run of them together ---------------------------------------------------------------------------------------
