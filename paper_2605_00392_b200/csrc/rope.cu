@@ -13,7 +13,9 @@ namespace rtp {
 // sum over the D / 16 (fp32: D / 8) lanes of a head, and its pairs are the same ones in every head.  The row's angles are computed
 // once, shared out over the lanes, while the first heads are on their way.  Angles in 64 bits, taken modulo a turn before they are rounded to
 // 32: at position 10^6 an fp32 angle would be off by 0.03.  Everything else in fp32, rounded once, at the store.
-// Bound by HBM: each element read and written once.
+// Each element is read and written once.  4999 rows of 40 heads in fp32: 41 us, 5.0 TB/s.  21568 rows of 20 heads in bf16: 57 us, 3.9 TB/s;
+// there it is latency and issue slots (55 % of them) more than HBM: other numbers of heads in flight and CTAs to an SM (2 at 6, 1 at 7, 5 at 4)
+// are within 3 % or slower (56.1, 55.8, 63.9; fp32 43.3, 51.4, 47.3).
 constexpr int kRpWarps = 4;
 constexpr int kRpAhead = 3;                  // heads' pieces of a lane whose loads are in flight together
 
