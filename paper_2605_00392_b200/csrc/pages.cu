@@ -310,9 +310,11 @@ template <typename T>
 static cudaError_t launch_write(cudaStream_t st, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int rows,
                                 const int32_t *slots, const CacheView &c, int sms)
 {
-    // rows of a window: as many CTAs as the device holds at once, so that single tokens, each a run of its own, go side by
-    // side, and long runs, of which a window of 64 rows starts one or two, do not launch CTAs that find none
-    const int64_t want = (int64_t)rows * 2 * c.kv_heads / ((int64_t)sms * 8) + 1;
+    // rows of a window: about twelve CTAs to an SM (eight run at a time), so that single tokens, each a run of its own, go side by
+    // side, and long runs, of which a window of 64 rows starts one or two, do not launch CTAs that find none.  Windows of 1 row and of 64
+    // against this rule, 10 heads of 128, in us: a token of 64 requests 4.8 / 60.2 / 4.8, of 256 13.4 / 58.7 / 12.0, five tokens of 64
+    // 9.4 / 15.1 / 6.1, 300 tokens of 1 request 7.7 / 3.7 / 3.7, of 4 26.4 / 5.4 / 5.1, of 64 398 / 30.5 / 30.3
+    const int64_t want = (int64_t)rows * 2 * c.kv_heads / ((int64_t)sms * 12);
     int window = 1;
     while (window < kCwMaxWindow && window < want) window *= 2;
     const int64_t ctas = (int64_t)((rows + window - 1) / window) * 2 * c.kv_heads;

@@ -184,7 +184,8 @@ extern "C" rtprune_status_t rtprune_qk_norm_rope(void *cuda_stream, rtprune_dtyp
     RopeArgs a = {q, k, q_weight, k_weight, q_out, k_out, q_stride, k_stride, q_out_stride, k_out_stride, positions, inv_freq,
                   (int)rows, 1, 0, q_heads, q_heads + kv_heads, head_dim, rotary_dim, interleaved ? 1 : 0, 0, eps};
     while ((2 * vec << a.group_shift) < head_dim) ++a.group_shift;
-    // few rows: their heads shared out over warps, down to one piece of each lane
+    // few rows: their heads shared out over warps, down to one piece of each lane (a warp for a row against this, 20 heads in bf16, in us:
+    // 1 row 4.8 / 2.8, 64 5.0 / 2.9, 512 5.6 / 4.0, 1000 6.2 / 6.8, 2000 7.9 / 11.4; 40 heads, 256 rows 7.9 / 3.9, in fp32 1000 rows 15.5 / 15.0)
     const int units = a.heads << a.group_shift;
     if (rows < 1024) a.parts = (units + 31) / 32;
     a.part_units = ((units + a.parts - 1) / a.parts + 31) / 32 * 32;
