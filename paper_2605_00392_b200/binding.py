@@ -7,6 +7,7 @@ loaded, or no CUDA device is present, the calls raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import numpy as np
 import os
 from dataclasses import dataclass
@@ -557,6 +558,7 @@ def cache_attend(q: torch.Tensor, offsets: torch.Tensor, seq_lens: torch.Tensor,
     return out
 
 
+@functools.lru_cache(maxsize=256)          # (sizes in, a size out: a call of 1.2 us)
 def cache_attend_workspace(batch: int, max_q_len: int, max_seq_len: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
     """rtprune_cache_attend_workspace: bytes of workspace a cache_attend of these sizes needs."""
     n = ctypes.c_size_t()
