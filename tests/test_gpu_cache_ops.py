@@ -117,7 +117,8 @@ def test_page_map_lengths_outside_the_contract(offsets, ctx):
     (1, 10, 10, 128, 128, False, True, 400), (7, 3, 1, 64, 64, False, True, 5000), (33, 32, 8, 128, 64, True, True, 120000),
     (5, 2, 2, 96, 96, False, True, 100), (9, 4, 2, 256, 256, True, False, 2 ** 31 - 1), (3, 1, 1, 16, 16, False, True, 9),
     (1300, 12, 4, 80, 32, False, True, 10 ** 6), (2, 5, 1, 128, 0, False, True, 9), (4, 0, 3, 48, 32, True, True, 99),
-    (3, 5, 0, 112, 112, False, True, 77), (2600, 10, 10, 128, 128, False, True, 450)])
+    (3, 5, 0, 112, 112, False, True, 77), (2600, 10, 10, 128, 128, False, True, 450),
+    (1000, 10, 10, 128, 128, False, True, 4000), (6100, 8, 2, 64, 32, True, True, 4000), (1023, 32, 8, 128, 128, False, False, 99)])
 def test_norm_rope(dtype, rows, qh, kh, dim, rot, inter, norm, far):
     gen = torch.Generator().manual_seed(rows + dim)
     pad = 3
@@ -141,6 +142,20 @@ def test_norm_rope(dtype, rows, qh, kh, dim, rot, inter, norm, far):
     binding.qk_norm_rope(q, k, pos.to(DEV), freq, wq, wk, 1e-5, interleaved=inter)                 # in place, in the fused rows
     assert torch.equal(q[:rows], q_out[:rows]) and torch.equal(k[:rows], k_out[:rows])
     assert torch.equal(x[rows:], before[rows:]) and torch.equal(x[:, (qh + kh) * dim:], before[:, (qh + kh) * dim:])
+
+
+@pytest.mark.parametrize("rows", [900, 4000])
+def test_norm_rope_passes_over_rows_of_no_request(rows):
+    # rows without a position between others, in place: left as they are, the others as without them
+    q, k = (torch.randn(rows, h, 128, generator=torch.Generator(DEV).manual_seed(h), device=DEV).to(torch.bfloat16) for h in (6, 2))
+    pos = torch.randint(0, 500, (rows,), generator=torch.Generator(DEV).manual_seed(1), device=DEV, dtype=torch.int32)
+    holes = torch.rand(rows, generator=torch.Generator(DEV).manual_seed(2), device=DEV) < 0.4
+    freq, w = binding.rope_frequencies(128, 1e4, DEV), torch.ones(128, dtype=torch.bfloat16, device=DEV)
+    all_q, all_k, some_q, some_k = q.clone(), k.clone(), q.clone(), k.clone()
+    binding.qk_norm_rope(all_q, all_k, pos, freq, w, w)
+    binding.qk_norm_rope(some_q, some_k, torch.where(holes, -1 - pos, pos), freq, w, w)
+    for before, whole, some in ((q, all_q, some_q), (k, all_k, some_k)):
+        assert torch.equal(some, torch.where(holes[:, None, None], before, whole))
 
 
 def test_norm_rope_zero_rows_of_zeros_and_not_finite():
