@@ -364,6 +364,17 @@ def test_attend_scales_far_apart_zero_and_large_scores(new, lens):
 
 
 @pytest.mark.usefixtures("bounds")
+@pytest.mark.parametrize("new", [[1, 1], [3, 40], [150, 2]])
+def test_attend_nothing_cached_and_a_scale_of_zero(new):
+    q, off, L, tables, cache = _batch(new, [60, 300], 4, 2, 64, 16, 12)
+    _check_attend(q, off, L, tables, cache, max(new), 300, scale=0.0, causal=False)
+    lse = torch.zeros(q.shape[:2], device=DEV)
+    out = binding.cache_attend(q, off, torch.zeros_like(L), tables[:, :0], cache, max_q_len=max(new), max_seq_len=0, out=torch.full_like(q, 2.0), lse=lse)
+    n = sum(new)
+    assert (out[:n] == 0).all() and (out[n:] == 2).all() and torch.isneginf(lse[:n]).all() and (lse[n:] == 0).all()
+
+
+@pytest.mark.usefixtures("bounds")
 @pytest.mark.parametrize("new,lens", [([1], [200]), ([5], [200]), ([150], [200])])
 def test_attend_queries_of_every_size(new, lens):
     q, off, L, tables, cache = _batch(new, lens, 4, 2, 128, 64, 9)
