@@ -655,23 +655,26 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
 // Puts the parts of tile (CTA blockIdx.x of the kernel above) together: a thread per row and four columns.
 template <int D>
 __global__ void __launch_bounds__(kArRows * D / 4)
-attend_join_kernel(const __grid_constant__ AttendArgs a, const float *__restrict__ part, const float2 *__restrict__ part_ml,
-                   const int4 *__restrict__ join)
+attend_join_kernel(const __grid_constant__ AttendArgs a, const float *part, const float2 *part_ml, const int4 *join)
 {
     ptx::grid_dep_launch();
     ptx::grid_dep_wait();
     const int4 what = join[blockIdx.x];
     const int r = threadIdx.x / (D / 4), col = threadIdx.x % (D / 4) * 4;
+    // the first two parts, which most joined tiles have and no more, are read beside the record that tells whether there are any: one trip to
+    // L2 instead of three (what is read of a tile that has none is not used)
+    const int next = min((int)blockIdx.x + 1, (int)gridDim.x - 1);
+    const int64_t at0 = (int64_t)(2 * blockIdx.x + 1) * kArRows + r, at1 = (int64_t)(2 * next) * kArRows + r;
+    const float2 ml0 = part_ml[at0], ml1 = part_ml[at1];
+    const float4 x0 = *reinterpret_cast<const float4 *>(part + at0 * D + col), x1 = *reinterpret_cast<const float4 *>(part + at1 * D + col);
     if (what.w == 0 || r >= (int)((uint32_t)what.z >> 26)) return;
-    float top = kAtNothing;
-    for (int p = 0; p < what.w; ++p) {
-        const int slot = 2 * (blockIdx.x + p) + (p == 0 ? 1 : 0);
-        top = fmaxf(top, part_ml[(int64_t)slot * kArRows + r].x);
-    }
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-    for (int p = 0; p < what.w; ++p) {
-        const int64_t at = (int64_t)(2 * (blockIdx.x + p) + (p == 0 ? 1 : 0)) * kArRows + r;
+    float top = fmaxf(ml0.x, ml1.x);
+    for (int p = 2; p < what.w; ++p) top = fmaxf(top, part_ml[(int64_t)(2 * (blockIdx.x + p)) * kArRows + r].x);
+    const float k0 = ex2(ml0.x - top), k1 = ex2(ml1.x - top);
+    float4 o = make_float4(fmaf(x1.x, k1, x0.x * k0), fmaf(x1.y, k1, x0.y * k0), fmaf(x1.z, k1, x0.z * k0), fmaf(x1.w, k1, x0.w * k0));
+    float l = fmaf(ml1.y, k1, ml0.y * k0);
+    for (int p = 2; p < what.w; ++p) {
+        const int64_t at = (int64_t)(2 * (blockIdx.x + p)) * kArRows + r;
         const float2 ml = part_ml[at];
         const float4 x = *reinterpret_cast<const float4 *>(part + at * D + col);
         const float k = ex2(ml.x - top);
