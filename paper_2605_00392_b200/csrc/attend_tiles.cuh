@@ -20,8 +20,8 @@
 // range, and the sums, which are needed anyway, show it with less work than a maximum (772 us against 805 for 37 requests of 512 rows
 // that see 8512 tokens).
 // Bound by the tensor cores and, about as much, by the exponentials: 128 x 128 scores take 1024 cycles of either (16 exponentials a
-// cycle and SM; two products of 128^3 at 4096 multiply-adds).  It takes 2200: 1.07 PFLOP/s at 512 rows over 8512 tokens, 224 us for 8 causal
-// requests of 2783 tokens and 99 us for 64 of 300 to 375, 10 heads.  Keys that need no conversion would make that 15 % less, a softmax
+// cycle and SM; two products of 128^3 at 4096 multiply-adds).  It takes 2200: 1.07 PFLOP/s at 512 rows over 8512 tokens, 211 us for 8 causal
+// requests of 2783 tokens and 97 us for 64 of 300 to 375, 10 heads.  Keys that need no conversion would make that 15 % less, a softmax
 // without arithmetic as much: both want the issue slots and the shared memory that the products read at its full rate.
 #pragma once
 #include "attend.cuh"
