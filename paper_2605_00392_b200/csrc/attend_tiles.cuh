@@ -18,7 +18,8 @@
 // 64 KB of queries, which need a line of it each while they are on their way, took 10,000 cycles.
 // A row's sums are rescaled only where 16 of its weights add up to more than 2^12 by the maximum so far: no weight has then left fp16's
 // range, and the sums, which are needed anyway, show it with less work than a maximum (772 us against 805 for 37 requests of 512 rows
-// that see 8512 tokens).
+// that see 8512 tokens).  A tile's rows behind the request's last (the next request's queries, or whatever shared memory held where a
+// token's heads do not divide 128) are computed like the others, but have no voice in how a warp goes on: a row's bits do not hang on them.
 // Bound by the tensor cores and, about as much, by the exponentials: 128 x 128 scores take 1024 cycles of either (16 exponentials a
 // cycle and SM; two products of 128^3 at 4096 multiply-adds).  It takes 2200: 1.07 PFLOP/s at 512 rows over 8512 tokens, 211 us for 8 causal
 // requests of 2783 tokens and 97 us for 64 of 300 to 375, 10 heads.  Keys that need no conversion would make that 15 % less, a softmax
@@ -599,7 +600,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                         const float to = fmaxf(top, now), k = ex2(top - to);
                         top = to;
                         l *= k;
-                        if (j > 0 && __any_sync(0xffffffffu, k < 1.f)) {
+                        if (j > 0 && __any_sync(0xffffffffu, mine >= 0 && k < 1.f)) {
 #pragma unroll 1
                             for (int c = 0; c < D / 16; ++c) {
                                 uint32_t o[16];
@@ -610,7 +611,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                                 tmem_st16(t_o + c * 16, o);
                             }
                         }
-                        careful = careful || __any_sync(0xffffffffu, fabsf(top) > kTlLarge);
+                        careful = careful || __any_sync(0xffffffffu, mine >= 0 && fabsf(top) > kTlLarge);
                     }
                     if (careful) {
                         careful_weights(group, factor, top, left, seen, t_s, l);
@@ -630,7 +631,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                     tile_weights(va, group + 4, factor, top, p + 32, most, more);
                     ptx::tmem_ld_wait();
                     tile_weights(vb, group + 6, factor, top, p + 48, most, more);
-                    if (!first && __any_sync(0xffffffffu, most > kTlSlack)) continue;
+                    if (!first && __any_sync(0xffffffffu, mine >= 0 && most > kTlSlack)) continue;
                     l += more;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_st16(t_s + 16 * c, *reinterpret_cast<uint32_t (*)[16]>(p + 16 * c));
