@@ -410,7 +410,7 @@ rtprune_status_t rtprune_cache_write(void *cuda_stream, rtprune_dtype_t dtype, c
  * Query head h reads kv head h / (q_heads / kv_heads).  A row that sees nothing gives out = 0, lse = -inf.  A row that sees a block of
  * scale NaN, or whose query is not finite, gives NaN (an infinite query may also give 0 or the values of its largest scores), and so does a row of a request that sees an entry of its table outside the cache or whose
  * seq_lens is outside 0 .. max_seq_len.  A request of more than max_q_len rows is passed over.  Values agree with those formulas in 64 bits to
- * the rounding of bf16; the softmax and all sums are fp32.  What a row's result is does not depend on the call's timing.
+ * the rounding of bf16, whatever the scales (0, or 2^-126 to 2^121, beside one another; never negative); the softmax and all sums are fp32.  What a row's result is does not depend on the call's timing.
  *
  *   q            DEVICE bf16 [rows] rows of q_heads heads of head_dim, 16-byte aligned, row stride in elements, a multiple of 8
  *   offsets      DEVICE int32 [batch+1], seq_lens DEVICE int32 [batch]; batch <= 65535

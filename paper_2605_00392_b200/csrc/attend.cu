@@ -32,7 +32,7 @@ static RowsLayout rows_layout(int ctas, int dim)
     RowsLayout w;
     w.part = 0;
     w.part_ml = w.part + (size_t)2 * ctas * kArRows * dim * 4;
-    w.join = w.part_ml + (size_t)2 * ctas * kArRows * 8;
+    w.join = w.part_ml + (size_t)2 * ctas * kArRows * 16;
     w.total = w.join + (size_t)ctas * 16;
     return w;
 }
@@ -93,10 +93,10 @@ static cudaError_t launch_rows(const AttendArgs &a, uint8_t *ws, cudaStream_t st
     if (e != cudaSuccess) return e;
     e = launch_chained(attend_rows_kernel<D, R>, dim3(whole ? (unsigned)tiles : (unsigned)ctas), dim3(kArThreads), (size_t)ArShape<D, R>::kSmem, st, a,
                        whole ? 1 : 0, (float *)(ws + w.part),
-                       (float2 *)(ws + w.part_ml), (int4 *)(ws + w.join));
+                       (float4 *)(ws + w.part_ml), (int4 *)(ws + w.join));
     if (e != cudaSuccess || whole) return e;
     return launch_chained(attend_join_kernel<D>, dim3(ctas), dim3(kArRows * D / 4), (size_t)0, st, a, (const float *)(ws + w.part),
-                          (const float2 *)(ws + w.part_ml), (const int4 *)(ws + w.join));
+                          (const float4 *)(ws + w.part_ml), (const int4 *)(ws + w.join));
 }
 
 // Items of the longest request that the call can have (it has no more rows than there are).

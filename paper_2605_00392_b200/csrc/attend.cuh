@@ -11,8 +11,14 @@
 // of two on
 //   s'_t = s_t log2(e) + log2(vs),  p'_t = 2^(s'_t - m'),  m' about the largest s' so far,
 // so that the values' scale is inside the weight (p' is what fp16 has to hold, and it is largest where the products are) and the
-// products are with bare codes; the sum of the softmax is that of p'_t / vs = 2^(s_t - m').  A block of scale 0
-// holds zeros: any log2(vs) does for it.
+// products are with bare codes; the sum of the softmax is that of p'_t / vs = 2^(s_t - m'), l.
+//
+// That holds while the scales that a row sees are within 2^80 of one another: from 2^-60 to 2^20.  Where a block's is outside (scales
+// may be anything from 2^-126 to 2^121), or is 0, a row goes on, to the end of its tile, with a second reference r about the largest s,
+//   l = sum_t 2^(s_t - r),  out = sum p' vc / l * 2^(m' - r),
+// because 2^(s_t - m') may pass fp32's range, and with a block's log2(vs) raised to m' - r - 80 in its weights: their p' are then 2^-80
+// and less, nothing in fp16, as what they stand for is, but still numbers of which p' / vs can be taken for l.  A block of zeros has no
+// log2(vs); one far below all others has it lead m' only where a row sees nothing else.
 #pragma once
 #include "serve.cuh"
 
@@ -33,7 +39,9 @@ struct AttendArgs {
 
 constexpr float kAtNothing = -1e30f;         // m' of a row that has seen nothing yet (finite: -inf minus it is still -inf)
 constexpr float kAtSlack = 8.f;              // m' follows the maximum only where a weight would pass 2^8 (fp16 ends at 2^16)
-constexpr float kAtZeroLog = -40.f;          // log2(vs) of a block of scale 0
+constexpr float kAtLowLog = -60.f, kAtHighLog = 20.f;      // log2(vs) for which l may have m' as its reference
+constexpr float kAtZeroLog = -200.f;         // log2(vs) of a block of scale 0
+constexpr float kAtLogGap = 80.f;
 constexpr float kAtLn2 = 0.69314718055994531f;
 
 // A request's rows and lengths.  false: it has no rows, or none that may be written.  len = -1: outside the contract, its rows
@@ -62,12 +70,17 @@ __device__ inline float ex2(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-// log2(vs) and 1 / vs of a block's scale.
-__device__ inline void value_scale(float vs, float &lv, float &inv)
+// log2(vs) and 1 / vs of a block's scale; true: one that m' does not do for as the reference of l.
+__device__ inline bool value_scale(float vs, float &lv, float &inv)
 {
     lv = vs == 0.f ? kAtZeroLog : __log2f(vs);
-    inv = vs == 0.f ? 1.0995116e12f : __frcp_rn(vs);
+    inv = __frcp_rn(vs);
+    return lv < kAtLowLog || lv > kAtHighLog;
 }
+// log2(vs) for the weights of a block, gap = m' - r.  (NaN stays.)
+__device__ inline float weight_log(float lv, float gap) { return lv < gap - kAtLogGap ? gap - kAtLogGap : lv; }
+// What a row's sums are multiplied by, twice: the root of 2^(m' - r), which may be as little as 2^-134.
+__device__ inline float half_gap(float m, float ref) { return ex2(0.5f * (m - ref)); }
 // Power of two that takes a row's largest |q| to [1, 4), and the factor of the row's scores that makes up for it (NaN where
 // the row is not finite).
 __device__ inline float query_scale(float top, float scale_log2, float &factor)

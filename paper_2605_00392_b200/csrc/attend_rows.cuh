@@ -177,19 +177,20 @@ __device__ inline uint32_t mat_trans(uint32_t x)
     return r;
 }
 
-// Parts of a tile that a cut goes through: `part` [2 per CTA][16][D] sums, `part_ml` [2 per CTA][16] (m', l).  A part that holds its
+// Parts of a tile that a cut goes through: `part` [2 per CTA][16][D] sums, `part_ml` [2 per CTA][16] (m', l, r).  A part that holds its
 // tile's first block is the CTA's second, any other its first.  join[CTA]: the tile that begins in the CTA and does not end in it:
 // (first row of the request, kv head, the tile's first row | its rows << 26, CTAs that it goes through; 0: there is none).
 template <int D, int R>
 __global__ void __launch_bounds__(kArThreads, ArShape<D, R>::kPerSm)
-attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float *__restrict__ part, float2 *__restrict__ part_ml, int4 *__restrict__ join)
+attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float *__restrict__ part, float4 *__restrict__ part_ml, int4 *__restrict__ join)
 {
     using S = ArShape<D, R>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ float row_factor[kArRows];
     __shared__ float2 row_ml[kArWarps][R];
-    __shared__ float4 scales[S::kStages][kArWarps];  // ks, log2 vs, 1 / vs of each warp's 16 tokens
+    __shared__ float row_ref[kArWarps][R];           // r of a warp's rows once they have one; infinity before (it is m' then)
+    __shared__ float4 scales[S::kStages][kArWarps];  // ks, log2 vs, 1 / vs of each warp's 16 tokens; w: 1 from the tile's first wide one on
     __shared__ uint64_t full[S::kStages], empty[S::kStages];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     const uint32_t ring = ptx::smem_u32(sm), frag = ring + S::kRing, scales_u32 = ptx::smem_u32(scales);
@@ -217,10 +218,13 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
         uint32_t n = 0;
         // of the step that is fetched, for the 16 tokens of warp lane / 8: their block (-1: none), and the codes' place in it
         int block = -1, slot = 0;
+        bool fresh = false, wide = false;            // a tile's first step (of this CTA); a scale so far wants a reference of its own for l
 #pragma unroll 1
         for (int look = 0; look <= todo; ++look) {
             int next_block = -1, next_slot = 0;
+            bool next_fresh = false;
             if (look < todo) {
+                next_fresh = at.block == 0;
                 const int t = at.block * kArBlock + (lane >> 3) * 16;
                 const int page = t < at.len ? attend_page(a, at.i, t) : -1;
                 next_block = page < 0 ? -1 : page * a.c.kv_heads + at.head;
@@ -248,14 +252,15 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
                 }
                 ptx::cp_async_arrive(&full[s]);
                 float lv, inv;
-                value_scale(vs, lv, inv);
-                if ((lane & 7) == 0) scales[s][lane >> 3] = make_float4(ks, lv, inv, 0.f);
+                wide = value_scale(vs, lv, inv) || (wide && !fresh);
+                if ((lane & 7) == 0) scales[s][lane >> 3] = make_float4(ks, lv, inv, wide ? 1.f : 0.f);
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&full[s]);
                 ++n;
             }
             block = next_block;
             slot = next_slot;
+            fresh = next_fresh;
         }
         ptx::cp_async_commit();
         ptx::cp_async_wait<0>();                     // no copy is left on its way into memory that this CTA gives back
@@ -358,6 +363,8 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
 #pragma unroll
         for (int j = 0; j < S::kNt; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
 
+        if (R == 8 ? g == 0 : c == 0) row_ref[warp][mine[0]] = row_ref[warp][mine[1]] = INFINITY;
+        __syncwarp();
         int t0 = first * kArBlock + warp * 16;
         uint32_t stage = n % S::kStages, parity = n / S::kStages & 1;
 #pragma unroll 1
@@ -383,44 +390,74 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
                     }
                     // ---- weights
                     const float k0 = f0 * sc.x, k1 = f1 * sc.x;
+                    if (t0 + 16 > lo_end || sc.w != 0.f) {
+                        // tokens that a row does not see, or a reference of its own for l, from here to the tile's end: the largest s and s'
+                        // are taken every time
+                        bool seen[4];
+                        float top_s[2], top[2], r[2];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[e] = fmaf(s[e], e & 1 ? k1 : k0, sc.y);
-                    const bool masked = t0 + 16 > lo_end;
-                    if (masked) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (t0 + g + 8 * (e >> 1) >= end[e & 1]) s[e] = -INFINITY;
-                    }
-                    const float top0 = fmaxf(s[0], s[2]), top1 = fmaxf(s[1], s[3]);
-                    if (__any_sync(0xffffffffu, fmaxf(top0 - m[0], top1 - m[1]) > kAtSlack)) {
-                        float n0 = top0, n1 = top1;
-#pragma unroll
-                        for (int o = 4; o < 32; o <<= 1) {
-                            n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, o));
-                            n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, o));
+                        for (int e = 0; e < 4; ++e) {
+                            s[e] *= e & 1 ? k1 : k0;
+                            seen[e] = t0 + g + 8 * (e >> 1) < end[e & 1];
                         }
-                        n0 = fmaxf(m[0], n0);
-                        n1 = fmaxf(m[1], n1);
-                        const float c0 = ex2(m[0] - n0), c1 = ex2(m[1] - n1);
-                        m[0] = n0;
-                        m[1] = n1;
-                        l[0] *= c0;
-                        l[1] *= c1;
 #pragma unroll
-                        for (int j = 0; j < S::kNt; ++j) {
-                            acc[j][0] *= c0;
-                            acc[j][1] *= c1;
-                            acc[j][2] *= c0;
-                            acc[j][3] *= c1;
+                        for (int x = 0; x < 2; ++x) {
+                            top_s[x] = fmaxf(seen[x] ? s[x] : -INFINITY, seen[2 + x] ? s[2 + x] : -INFINITY);
+#pragma unroll
+                            for (int o = 4; o < 32; o <<= 1) top_s[x] = fmaxf(top_s[x], __shfl_xor_sync(0xffffffffu, top_s[x], o));
+                            r[x] = row_ref[warp][mine[x]];
+                            if (r[x] == INFINITY) r[x] = m[x];
+                            top[x] = fmaxf(m[x], top_s[x] + sc.y);
+                            const float to = fmaxf(r[x], top_s[x]), k = ex2(m[x] - top[x]);
+                            l[x] *= ex2(r[x] - to);
+                            m[x] = top[x];
+                            r[x] = to;
+#pragma unroll
+                            for (int j = 0; j < S::kNt; ++j) {
+                                acc[j][x] *= k;
+                                acc[j][x + 2] *= k;
+                            }
                         }
-                    }
+                        __syncwarp();
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[e] = ex2(s[e] - m[e & 1]);
-                    {
-                        const float p0 = s[0] + s[2], p1 = s[1] + s[3];
-                        // weights of 0 add nothing, whatever the block's scale is (of one that the row does not see)
-                        if (!masked || p0 != 0.f) l[0] = fmaf(p0, sc.z, l[0]);
-                        if (!masked || p1 != 0.f) l[1] = fmaf(p1, sc.z, l[1]);
+                        for (int x = 0; x < 2; ++x) {
+                            if (g == 0) row_ref[warp][mine[x]] = r[x];
+                            const float gap = m[x] - r[x], lv = weight_log(sc.y, gap);
+                            s[x] = seen[x] ? ex2(s[x] + lv - m[x]) : 0.f;
+                            s[2 + x] = seen[2 + x] ? ex2(s[2 + x] + lv - m[x]) : 0.f;
+                            if (seen[x] || seen[2 + x]) l[x] = fmaf(s[x] + s[2 + x], ex2(gap - lv), l[x]);
+                        }
+                        __syncwarp();
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[e] = fmaf(s[e], e & 1 ? k1 : k0, sc.y);
+                        const float top0 = fmaxf(s[0], s[2]), top1 = fmaxf(s[1], s[3]);
+                        if (__any_sync(0xffffffffu, fmaxf(top0 - m[0], top1 - m[1]) > kAtSlack)) {
+                            float n0 = top0, n1 = top1;
+#pragma unroll
+                            for (int o = 4; o < 32; o <<= 1) {
+                                n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, o));
+                                n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, o));
+                            }
+                            n0 = fmaxf(m[0], n0);
+                            n1 = fmaxf(m[1], n1);
+                            const float c0 = ex2(m[0] - n0), c1 = ex2(m[1] - n1);
+                            m[0] = n0;
+                            m[1] = n1;
+                            l[0] *= c0;
+                            l[1] *= c1;
+#pragma unroll
+                            for (int j = 0; j < S::kNt; ++j) {
+                                acc[j][0] *= c0;
+                                acc[j][1] *= c1;
+                                acc[j][2] *= c0;
+                                acc[j][3] *= c1;
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[e] = ex2(s[e] - m[e & 1]);
+                        l[0] = fmaf(s[0] + s[2], sc.z, l[0]);
+                        l[1] = fmaf(s[1] + s[3], sc.z, l[1]);
                     }
                     const uint32_t b0 = mat_trans(pack_half(s[0], s[1])), b1 = mat_trans(pack_half(s[2], s[3]));
                     // ---- values: tokens 2c, 2c + 1, 2c + 8, 2c + 9, columns D / 8 * g ..: mma tile j has columns 2j and 2j + 1 of these
@@ -472,46 +509,72 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
                     }
                     // ---- weights
                     const float k0 = f0 * sc.x, k1 = f1 * sc.x;
+                    if (t0 + 16 > lo_end || sc.w != 0.f) {
+                        // tokens that a row does not see, or a reference of its own for l, from here to the tile's end: the largest s and s'
+                        // are taken every time
 #pragma unroll
-                    for (int x = 0; x < 2; ++x)
+                        for (int h = 0; h < 2; ++h) {        // row g + 8 h: its scores are s[0][2h], s[0][2h + 1], s[1][2h], s[1][2h + 1]
+                            float top_s = -INFINITY;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[x][e] = fmaf(s[x][e], e < 2 ? k0 : k1, sc.y);
-                    const bool masked = t0 + 16 > lo_end;
-                    if (masked) {
+                            for (int e = 0; e < 4; ++e) {
+                                float &x = s[e >> 1][2 * h + (e & 1)];
+                                x *= h ? k1 : k0;
+                                if (t0 + 8 * (e >> 1) + 2 * c + (e & 1) < end[h]) top_s = fmaxf(top_s, x);
+                            }
+                            top_s = fmaxf(top_s, __shfl_xor_sync(0xffffffffu, top_s, 1));
+                            top_s = fmaxf(top_s, __shfl_xor_sync(0xffffffffu, top_s, 2));
+                            float r = row_ref[warp][mine[h]];
+                            if (r == INFINITY) r = m[h];
+                            const float top = fmaxf(m[h], top_s + sc.y), to = fmaxf(r, top_s), k = ex2(m[h] - top);
+                            l[h] *= ex2(r - to);
+                            m[h] = top;
+#pragma unroll
+                            for (int j = 0; j < S::kNt; ++j) {
+                                acc[j][2 * h] *= k;
+                                acc[j][2 * h + 1] *= k;
+                            }
+                            __syncwarp();
+                            if (c == 0) row_ref[warp][mine[h]] = to;
+                            __syncwarp();
+                            const float gap = top - to, lv = weight_log(sc.y, gap), z = ex2(gap - lv);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                float &x = s[e >> 1][2 * h + (e & 1)];
+                                const bool seen = t0 + 8 * (e >> 1) + 2 * c + (e & 1) < end[h];
+                                x = seen ? ex2(x + lv - top) : 0.f;
+                                if (seen) l[h] = fmaf(x, z, l[h]);
+                            }
+                        }
+                    } else {
 #pragma unroll
                         for (int x = 0; x < 2; ++x)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (t0 + 8 * x + 2 * c + (e & 1) >= end[e >> 1]) s[x][e] = -INFINITY;
-                    }
-                    const float top0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
-                    const float top1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
-                    if (__any_sync(0xffffffffu, fmaxf(top0 - m[0], top1 - m[1]) > kAtSlack)) {
-                        float n0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, 1)), n1 = fmaxf(top1, __shfl_xor_sync(0xffffffffu, top1, 1));
-                        n0 = fmaxf(m[0], fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, 2)));
-                        n1 = fmaxf(m[1], fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, 2)));
-                        const float c0 = ex2(m[0] - n0), c1 = ex2(m[1] - n1);
-                        m[0] = n0;
-                        m[1] = n1;
-                        l[0] *= c0;
-                        l[1] *= c1;
+                            for (int e = 0; e < 4; ++e) s[x][e] = fmaf(s[x][e], e < 2 ? k0 : k1, sc.y);
+                        const float top0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
+                        const float top1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
+                        if (__any_sync(0xffffffffu, fmaxf(top0 - m[0], top1 - m[1]) > kAtSlack)) {
+                            float n0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, 1)), n1 = fmaxf(top1, __shfl_xor_sync(0xffffffffu, top1, 1));
+                            n0 = fmaxf(m[0], fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, 2)));
+                            n1 = fmaxf(m[1], fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, 2)));
+                            const float c0 = ex2(m[0] - n0), c1 = ex2(m[1] - n1);
+                            m[0] = n0;
+                            m[1] = n1;
+                            l[0] *= c0;
+                            l[1] *= c1;
 #pragma unroll
-                        for (int j = 0; j < S::kNt; ++j) {
-                            acc[j][0] *= c0;
-                            acc[j][1] *= c0;
-                            acc[j][2] *= c1;
-                            acc[j][3] *= c1;
+                            for (int j = 0; j < S::kNt; ++j) {
+                                acc[j][0] *= c0;
+                                acc[j][1] *= c0;
+                                acc[j][2] *= c1;
+                                acc[j][3] *= c1;
+                            }
                         }
-                    }
 #pragma unroll
-                    for (int x = 0; x < 2; ++x)
+                        for (int x = 0; x < 2; ++x)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[x][e] = ex2(s[x][e] - m[e >> 1]);
-                    {
-                        const float p0 = (s[0][0] + s[0][1]) + (s[1][0] + s[1][1]), p1 = (s[0][2] + s[0][3]) + (s[1][2] + s[1][3]);
-                        // weights of 0 add nothing, whatever the block's scale is (of one that the row does not see)
-                        if (!masked || p0 != 0.f) l[0] = fmaf(p0, sc.z, l[0]);
-                        if (!masked || p1 != 0.f) l[1] = fmaf(p1, sc.z, l[1]);
+                            for (int e = 0; e < 4; ++e) s[x][e] = ex2(s[x][e] - m[e >> 1]);
+                        l[0] = fmaf((s[0][0] + s[0][1]) + (s[1][0] + s[1][1]), sc.z, l[0]);
+                        l[1] = fmaf((s[0][2] + s[0][3]) + (s[1][2] + s[1][3]), sc.z, l[1]);
                     }
                     const uint4 pf = make_uint4(pack_half(s[0][0], s[0][1]), pack_half(s[0][2], s[0][3]), pack_half(s[1][0], s[1][1]),
                                                 pack_half(s[1][2], s[1][3]));
@@ -556,21 +619,25 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
             // over the lanes of a row: the four of a g, or the eight of a c
 #pragma unroll
             for (int o = R == 8 ? 4 : 1; o < (R == 8 ? 32 : 4); o <<= 1) l[x] += __shfl_xor_sync(0xffffffffu, l[x], o);
-            if (R == 8 ? g == 0 : c == 0) row_ml[warp][mine[x]] = make_float2(m[x], l[x]);
+            if (R == 8 ? g == 0 : c == 0) {
+                row_ml[warp][mine[x]] = make_float2(m[x], l[x]);
+                if (row_ref[warp][mine[x]] == INFINITY) row_ref[warp][mine[x]] = m[x];
+            }
         }
         ar_sync();
-        float sum_l[2];
+        float sum_l[2], ref[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             float top = kAtNothing;
-#pragma unroll
-            for (int w = 0; w < kArWarps; ++w) top = fmaxf(top, row_ml[w][mine[x]].x);
-            sum_l[x] = 0.f;
+            ref[x] = kAtNothing;
 #pragma unroll
             for (int w = 0; w < kArWarps; ++w) {
-                const float2 ml = row_ml[w][mine[x]];
-                sum_l[x] += ml.y * ex2(ml.x - top);
+                top = fmaxf(top, row_ml[w][mine[x]].x);
+                ref[x] = fmaxf(ref[x], row_ref[w][mine[x]]);
             }
+            sum_l[x] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kArWarps; ++w) sum_l[x] += row_ml[w][mine[x]].y * ex2(row_ref[w][mine[x]] - ref[x]);
             const float k = ex2(m[x] - top);
             m[x] = top;
 #pragma unroll
@@ -616,7 +683,8 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
                 const bool lead = R == 8 ? g == 0 : c == 0;
                 if (whole) {
                     const bool nan = at.len < 0;
-                    const float k = nan ? __uint_as_float(0x7fc00000u) : sum_l[x] == 0.f ? 0.f : 1.f / sum_l[x];
+                    const float half = half_gap(m[x], ref[x]);
+                    const float k = nan ? __uint_as_float(0x7fc00000u) : sum_l[x] == 0.f ? 0.f : 1.f / sum_l[x] * half;
                     const int j = mr / a.group;
                     const int64_t o = (int64_t)(at.row0 + j) * a.q_heads + at.head * a.group + (mr - j * a.group);
                     __nv_bfloat16 *to = a.out + o * D + col;
@@ -625,17 +693,17 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
                         uint4 w;
                         __nv_bfloat162 *h = reinterpret_cast<__nv_bfloat162 *>(&w);
 #pragma unroll
-                        for (int z = 0; z < 4; ++z) h[z] = __floats2bfloat162_rn(value(x, e + 2 * z) * k, value(x, e + 2 * z + 1) * k);
+                        for (int z = 0; z < 4; ++z) h[z] = __floats2bfloat162_rn(value(x, e + 2 * z) * k * half, value(x, e + 2 * z + 1) * k * half);
                         *reinterpret_cast<uint4 *>(to + e) = w;
                     }
-                    if (a.lse && lead) a.lse[o] = nan ? k : sum_l[x] == 0.f ? -INFINITY : (m[x] + log2f(sum_l[x])) * kAtLn2;
+                    if (a.lse && lead) a.lse[o] = nan ? k : sum_l[x] == 0.f ? -INFINITY : (ref[x] + log2f(sum_l[x])) * kAtLn2;
                 } else {
                     const int slot = 2 * blockIdx.x + (first == 0 ? 1 : 0);
                     float *to = part + ((int64_t)slot * kArRows + r) * D + col;
 #pragma unroll
                     for (int e = 0; e < kCols; e += 4)
                         *reinterpret_cast<float4 *>(to + e) = make_float4(value(x, e), value(x, e + 1), value(x, e + 2), value(x, e + 3));
-                    if (lead) part_ml[(int64_t)slot * kArRows + r] = make_float2(m[x], sum_l[x]);
+                    if (lead) part_ml[(int64_t)slot * kArRows + r] = make_float4(m[x], sum_l[x], ref[x], 0.f);
                 }
             }
         }
@@ -655,7 +723,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
 // Puts the parts of tile (CTA blockIdx.x of the kernel above) together: a thread per row and four columns.
 template <int D>
 __global__ void __launch_bounds__(kArRows * D / 4)
-attend_join_kernel(const __grid_constant__ AttendArgs a, const float *part, const float2 *part_ml, const int4 *join)
+attend_join_kernel(const __grid_constant__ AttendArgs a, const float *part, const float4 *part_ml, const int4 *join)
 {
     ptx::grid_dep_launch();
     ptx::grid_dep_wait();
@@ -665,20 +733,24 @@ attend_join_kernel(const __grid_constant__ AttendArgs a, const float *part, cons
     // L2 instead of three (what is read of a tile that has none is not used)
     const int next = min((int)blockIdx.x + 1, (int)gridDim.x - 1);
     const int64_t at0 = (int64_t)(2 * blockIdx.x + 1) * kArRows + r, at1 = (int64_t)(2 * next) * kArRows + r;
-    const float2 ml0 = part_ml[at0], ml1 = part_ml[at1];
+    const float4 ml0 = part_ml[at0], ml1 = part_ml[at1];
     const float4 x0 = *reinterpret_cast<const float4 *>(part + at0 * D + col), x1 = *reinterpret_cast<const float4 *>(part + at1 * D + col);
     if (what.w == 0 || r >= (int)((uint32_t)what.z >> 26)) return;
-    float top = fmaxf(ml0.x, ml1.x);
-    for (int p = 2; p < what.w; ++p) top = fmaxf(top, part_ml[(int64_t)(2 * (blockIdx.x + p)) * kArRows + r].x);
+    float top = fmaxf(ml0.x, ml1.x), ref = fmaxf(ml0.z, ml1.z);
+    for (int p = 2; p < what.w; ++p) {
+        const float4 ml = part_ml[(int64_t)(2 * (blockIdx.x + p)) * kArRows + r];
+        top = fmaxf(top, ml.x);
+        ref = fmaxf(ref, ml.z);
+    }
     const float k0 = ex2(ml0.x - top), k1 = ex2(ml1.x - top);
     float4 o = make_float4(fmaf(x1.x, k1, x0.x * k0), fmaf(x1.y, k1, x0.y * k0), fmaf(x1.z, k1, x0.z * k0), fmaf(x1.w, k1, x0.w * k0));
-    float l = fmaf(ml1.y, k1, ml0.y * k0);
+    float l = fmaf(ml1.y, ex2(ml1.z - ref), ml0.y * ex2(ml0.z - ref));
     for (int p = 2; p < what.w; ++p) {
         const int64_t at = (int64_t)(2 * (blockIdx.x + p)) * kArRows + r;
-        const float2 ml = part_ml[at];
+        const float4 ml = part_ml[at];
         const float4 x = *reinterpret_cast<const float4 *>(part + at * D + col);
         const float k = ex2(ml.x - top);
-        l = fmaf(ml.y, k, l);
+        l = fmaf(ml.y, ex2(ml.z - ref), l);
         o.x = fmaf(x.x, k, o.x);
         o.y = fmaf(x.y, k, o.y);
         o.z = fmaf(x.z, k, o.z);
@@ -686,13 +758,13 @@ attend_join_kernel(const __grid_constant__ AttendArgs a, const float *part, cons
     }
     const int m = (what.z & 0x3ffffff) + r, j = m / a.group;
     const int64_t row = (int64_t)(what.x + j) * a.q_heads + what.y * a.group + (m - j * a.group);
-    const float k = l == 0.f ? 0.f : 1.f / l;
+    const float half = half_gap(top, ref), k = l == 0.f ? 0.f : 1.f / l * half;
     uint2 w;
     __nv_bfloat162 *h = reinterpret_cast<__nv_bfloat162 *>(&w);
-    h[0] = __floats2bfloat162_rn(o.x * k, o.y * k);
-    h[1] = __floats2bfloat162_rn(o.z * k, o.w * k);
+    h[0] = __floats2bfloat162_rn(o.x * k * half, o.y * k * half);
+    h[1] = __floats2bfloat162_rn(o.z * k * half, o.w * k * half);
     *reinterpret_cast<uint2 *>(a.out + row * D + col) = w;
-    if (a.lse && col == 0) a.lse[row] = l == 0.f ? -INFINITY : (top + log2f(l)) * kAtLn2;
+    if (a.lse && col == 0) a.lse[row] = l == 0.f ? -INFINITY : (ref + log2f(l)) * kAtLn2;
 }
 
 }  // namespace rtp

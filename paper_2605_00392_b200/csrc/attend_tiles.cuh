@@ -60,7 +60,9 @@ constexpr int kTlReaders = 15;                       // warps that read them
 constexpr int kTlGroupRing = 8;
 
 struct TlShared {
-    float4 group[kTlGroupRing][kTlGroups];           // ks, log2 vs, 1 / vs of each 16 tokens of the line's n-th block at n mod kTlGroupRing
+    // ks, log2 vs, 1 / vs of each 16 tokens of the line's n-th block at n mod kTlGroupRing; w: infinity if any of the block's scales wants
+    // a reference of its own for l, else 0
+    float4 group[kTlGroupRing][kTlGroups];
     TlItem item[kTlItems];
     uint64_t item_full[kTlItems], item_empty[kTlItems];
     uint64_t code_full[4], code_empty[4];            // keys of block 0, values of block 0, keys of block 1, ...
@@ -235,10 +237,12 @@ __device__ inline void tile_weights(const uint32_t (&v)[32], const float4 *group
     }
 }
 // The same where tokens from `left` on are not seen, or scores are so large that their own rounding matters: it is what the maximum
-// went through, so they go through it too before the maximum is taken off.  Loops of few instructions, from TMEM again.
-__device__ inline float careful_top(const float4 *group, float factor, int left, int seen, uint32_t t_s)
+// went through, so they go through it too before the maximum is taken off; or where l has a reference of its own (now_s: the largest s;
+// gap = top - ref, 0 where it has not).  Loops of few instructions, from TMEM again.
+__device__ inline float careful_top(const float4 *group, float factor, int left, int seen, uint32_t t_s, float &now_s)
 {
     float now = kAtNothing;
+    now_s = kAtNothing;
 #pragma unroll 1
     for (int c = 0; 32 * c < seen; ++c, left -= 32) {
         uint32_t v[32];
@@ -250,12 +254,14 @@ __device__ inline float careful_top(const float4 *group, float factor, int left,
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = 16 * h + e < left ? __uint_as_float(v[16 * h + e]) : -INFINITY;
             const float4 g = group[2 * c + h];
-            now = fmaxf(now, fmaf(max16(s), factor * g.x, g.y));
+            const float most = max16(s), k = factor * g.x;
+            now = fmaxf(now, fmaf(most, k, g.y));
+            now_s = fmaxf(now_s, most * k);
         }
     }
     return now;
 }
-__device__ inline void careful_weights(const float4 *group, float factor, float top, int left, int seen, uint32_t t_s, float &l)
+__device__ inline void careful_weights(const float4 *group, float factor, float top, float gap, int left, int seen, uint32_t t_s, float &l)
 {
 #pragma unroll 1
     for (int c = 0; c < kTlBlock / 32; ++c, left -= 32) {
@@ -266,17 +272,17 @@ __device__ inline void careful_weights(const float4 *group, float factor, float 
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const float4 g = group[2 * c + h];
-                const float k = factor * g.x;
+                const float k = factor * g.x, lv = weight_log(g.y, gap);
                 float w[16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) w[e] = ex2(fmaf(__uint_as_float(v[16 * h + e]), k, g.y) - top);
+                for (int e = 0; e < 16; ++e) w[e] = ex2(fmaf(__uint_as_float(v[16 * h + e]), k, lv) - top);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) w[e] = 16 * h + e < left ? w[e] : 0.f;
                 const float sum = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])) + (((w[8] + w[9]) + (w[10] + w[11])) + ((w[12] + w[13]) + (w[14] + w[15])));
 #pragma unroll
                 for (int e = 0; e < 8; ++e) p[8 * h + e] = pack_half(w[2 * e], w[2 * e + 1]);
                 // weights of 0 add nothing, whatever the block's scale is (of a page that the row does not see)
-                if (sum != 0.f) l = fmaf(sum, g.z, l);
+                if (sum != 0.f) l = fmaf(sum, ex2(gap - lv), l);
             }
         } else {
 #pragma unroll
@@ -432,8 +438,9 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                         const int64_t block = (int64_t)max(page_g, 0) * a.c.kv_heads + t.head;
                         const float nan = __uint_as_float(0x7fc00000u);
                         float lv, inv;
-                        value_scale(page_g < 0 ? nan : __ldg(a.c.v_scale + block), lv, inv);
-                        sh->group[n % kTlGroupRing][lane] = make_float4(page_g < 0 ? nan : __ldg(a.c.k_scale + block), lv, inv, 0.f);
+                        const bool wide = value_scale(page_g < 0 ? nan : __ldg(a.c.v_scale + block), lv, inv);
+                        const bool any = __any_sync((1u << kTlGroups) - 1u, wide);
+                        sh->group[n % kTlGroupRing][lane] = make_float4(page_g < 0 ? nan : __ldg(a.c.k_scale + block), lv, inv, any ? INFINITY : 0.f);
                     }
                     const uint32_t bytes = (uint32_t)(__popc(__ballot_sync(0xffffffffu, page >= 0)) * per_page * D);
                     const int64_t from = ((int64_t)max(page, 0) * a.c.kv_heads + t.head) * a.c.page_size * D;
@@ -568,7 +575,8 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         bool has = false, bad = false;
 #pragma unroll 1
         for (uint32_t item = 0;; ++item) {
-            float top = kAtNothing, l = 0.f;
+            float top = kAtNothing, ref = kAtNothing, l = 0.f;   // m', r (what l is relative to: m' until a block is wide)
+            bool wide = false;
             const int warp_most = __shfl_sync(0xffffffffu, end, 31), warp_end = __shfl_sync(0xffffffffu, end, 0);   // (the first row sees the fewest tokens)
 #pragma unroll 1
             for (int j = 0; ok && j < blocks; ++j, ++turns) {
@@ -578,14 +586,15 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                 const int left = end - j * kTlBlock; // tokens of the block that the row sees
                 const bool masked = (j + 1) * kTlBlock > warp_end;
                 const int seen = min(warp_most - j * kTlBlock, kTlBlock);
-                bool careful = masked;
+                bool careful = masked || wide;
                 // Weights against the maximum so far, in one pass; only where a row has one that is too large for fp16 by it (or nothing
                 // yet: the first block) its maximum is looked for first
-                for (bool first = j == 0 || masked;; first = true) {
+                for (bool first = j == 0 || careful;; first = true) {
                     if (first) {
-                        float now = kAtNothing;      // the row's maximum (of s', with the values' scale)
+                        if (group[0].w != 0.f) wide = careful = true;    // from here on, for the item
+                        float now = kAtNothing, now_s = kAtNothing;      // the row's maximum (of s', with the values' scale), and that of s
                         if (careful) {
-                            now = careful_top(group, factor, left, seen, t_s);
+                            now = careful_top(group, factor, left, seen, t_s, now_s);
                         } else {
 #pragma unroll 1
                             for (int c = 0; c < 4; c += 2) {
@@ -599,7 +608,9 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                         }
                         const float to = fmaxf(top, now), k = ex2(top - to);
                         top = to;
-                        l *= k;
+                        const float r = wide ? fmaxf(ref, now_s) : to;
+                        l *= ex2(ref - r);
+                        ref = r;
                         if (j > 0 && __any_sync(0xffffffffu, mine >= 0 && k < 1.f)) {
 #pragma unroll 1
                             for (int c = 0; c < D / 16; ++c) {
@@ -614,11 +625,11 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                         careful = careful || __any_sync(0xffffffffu, mine >= 0 && fabsf(top) > kTlLarge);
                     }
                     if (careful) {
-                        careful_weights(group, factor, top, left, seen, t_s, l);
+                        careful_weights(group, factor, top, top - ref, left, seen, t_s, l);
                         break;
                     }
                     uint32_t va[32], vb[32], p[64];
-                    float most = 0.f, more = 0.f;
+                    float most = group[0].w, more = 0.f;         // (a wide block: infinity)
                     ptx::tmem_ld32(t_s, va);
                     ptx::tmem_ld_wait();
                     ptx::tmem_ld32(t_s + 32, vb);
@@ -665,7 +676,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                 if (!ok) sh->gave_up = 1;
                 ptx::tc_fence_after();
                 const bool nan = bad || sh->gave_up;
-                const float k = nan ? __uint_as_float(0x7fc00000u) : l == 0.f ? 0.f : 1.f / l;
+                const float half = half_gap(top, ref), k = nan ? __uint_as_float(0x7fc00000u) : l == 0.f ? 0.f : 1.f / l * half;
                 __nv_bfloat16 *to = a.out + (int64_t)max(mine, 0) * D;
 #pragma unroll 1
                 for (int b = 0; b < D / 32; ++b) {
@@ -679,7 +690,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                     uint32_t o[16];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(v[2 * e]) * k, __uint_as_float(v[2 * e + 1]) * k);
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(v[2 * e]) * k * half, __uint_as_float(v[2 * e + 1]) * k * half);
                         o[e] = any || nan ? *reinterpret_cast<const uint32_t *>(&h) : 0u;      // a tile that saw no block has no sums
                     }
                     if (mine >= 0) {
@@ -687,7 +698,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                         st_global_v8(to + b * 32 + 16, o + 8);
                     }
                 }
-                if (mine >= 0 && a.lse) a.lse[mine] = nan ? k : l == 0.f ? -INFINITY : (top + log2f(l)) * kAtLn2;
+                if (mine >= 0 && a.lse) a.lse[mine] = nan ? k : l == 0.f ? -INFINITY : (ref + log2f(l)) * kAtLn2;
             }
             if (next.i < 0) break;
             has = true;

@@ -8,7 +8,7 @@ import torch
 
 import cache_ref as ref
 from paper_2605_00392_b200 import binding
-from test_gpu_cache_ops import DEV, _batch, _i32, bounds  # noqa: F401  (a fixture)
+from test_gpu_cache_ops import DEV, _batch, _i32, bounds  # noqa: F401  (bounds: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +53,92 @@ def test_attend_whatever_the_kernel_before_left_in_shared_memory(group, dim):
         binding.cache_attend(x, *fill[1:], max_q_len=256, max_seq_len=256)           # every SM, every row of its tiles
         got.append(binding.cache_attend(q, off, L, tables, cache, max_q_len=MANY, max_seq_len=length)[:n])
     assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+
+
+# ---- attention: scales of values at the ends of their range ------------------------------------------------------------
+
+def _check_tight(q, off, L, tables, cache, max_q, max_len, causal=True):
+    """As the formulas in 64 bits, with no absolute allowance but half of bf16's smallest number, so that values of any size count.
+    (Each term as in test_gpu_cache_ops: the output's rounding; weights in fp16, 2^-11, and fp32 sums; the score's error; weights that
+    are subnormal in fp16.)"""
+    lse = torch.zeros(q.shape[:2], device=DEV)
+    out = binding.cache_attend(q, off, L, tables, cache, max_q_len=max_q, max_seq_len=max_len, causal=causal, lse=lse)
+    want, wlse, weight, dots, least = ref.attend(q.cpu(), off.tolist(), L.tolist(), tables.cpu(), [t.cpu() for t in cache], q.shape[2] ** -0.5, causal)
+    n = int(off[-1])
+    want, wlse, weight, dots, least = want[:n], wlse[:n], weight[:n], dots[:n], least[:n]
+    err = (2.0 ** -17 * dots)[..., None]
+    bound = 2.0 ** -8 * want.abs() + (2.0 ** -10 + 2 * err) * weight + 2.0 ** -25 * least + 2.0 ** -134
+    got, glse = out[:n].cpu().double(), lse[:n].cpu().double()
+    assert torch.isfinite(got).all() and torch.isfinite(glse).all()
+    assert ((got - want).abs() <= bound).all(), ((got - want).abs() / bound).max()
+    assert ((glse - wlse).abs() <= err[..., 0] + 2.0 ** -20 * (1 + wlse.abs())).all()
+
+
+def _pattern(name, pages, gen):
+    """log2 of each page's scale of values; None: a page of zeros."""
+    at = list(range(pages))
+    if name == "least":
+        return [-126] * pages
+    if name == "most":
+        return [121] * pages
+    if name == "one_ordinary":
+        return [-5] + [-126] * (pages - 1)
+    if name == "ordinary_last":
+        return [-126] * (pages - 1) + [-5]
+    if name == "zero_beside_small":
+        return [None if i % 3 == 0 else -66 for i in at]
+    if name == "zeros_then_least":
+        return [None if i < pages // 2 else -126 for i in at]
+    if name == "zeros":
+        return [None] * pages
+    if name == "ends":
+        return [(-126, 121, -5, None)[i % 4] for i in at]
+    if name == "ends_once":
+        return [-126] * (pages - 1) + [121]
+    return [int(x) for x in torch.randint(-126, 122, (pages,), generator=gen)]
+
+
+@pytest.mark.usefixtures("bounds")
+@pytest.mark.parametrize("name", ["least", "most", "one_ordinary", "ordinary_last", "zero_beside_small", "zeros_then_least", "zeros", "ends", "ends_once", "any"])
+@pytest.mark.parametrize("new,lens,qh,kh,dim,page", [([1, 1], [1000, 77], 4, 4, 128, 16), ([5], [300], 8, 2, 64, 16), ([1], [3000], 4, 1, 128, 64),
+                                                     ([20, 3], [700, 5], 4, 2, 128, 32), ([150], [640], 2, 2, 128, 16), ([140], [400], 3, 1, 64, 64)])
+def test_attend_scales_at_the_ends_of_their_range(new, lens, qh, kh, dim, page, name):
+    q, off, L, tables, cache = _batch(new, lens, qh, kh, dim, page, 17)
+    gen = torch.Generator().manual_seed(len(name))
+    for i, length in enumerate(lens):
+        ids = tables[i, :-(-length // page)].long()
+        for p, e in zip(ids.tolist(), _pattern(name, ids.numel(), gen)):
+            cache.v_scale[p] = 0.0 if e is None else 2.0 ** e
+            if e is None:
+                cache.v[p] = 0
+    for x in (torch.zeros_like(q), q, 8 * q):               # equal scores; ordinary ones; some 2^50 apart
+        _check_tight(x, off, L, tables, cache, max(new), max(lens))
+
+
+@pytest.mark.usefixtures("bounds")
+@pytest.mark.parametrize("new", [[1], [150]])
+def test_attend_many_small_values_beside_an_ordinary_one(new):
+    # a page of ordinary values and score 0, a thousand tokens of values near 2^-126 with a score of -6 in powers of two: 15.6 of the sum's 16.6
+    q, off, L, tables, cache = _batch(new, [1024], 1, 1, 64, 16, 5)
+    q.fill_(1.0)
+    cache.k.fill_(-1)
+    cache.k_scale.fill_(6 * math.log(2) / 64 * 8)           # q . k = -6 ln 2 / scale
+    cache.v_scale.fill_(2.0 ** -126)
+    first = tables[0, 0].long()
+    cache.k[first], cache.v_scale[first] = 0, 2.0 ** -5
+    _check_tight(q, off, L, tables, cache, max(new), 1024, causal=False)
+    _check_tight(q, off, L, tables, cache, max(new), 1024)
+
+
+@pytest.mark.usefixtures("bounds")
+@pytest.mark.parametrize("x", [1.4e-36, 1e-30, 3e37])
+def test_written_values_of_any_size_are_read_back(x):
+    # through the cache write: rows of one value, equal scores: the value comes out
+    cache = binding.PagedCache.allocate(40, 2, 16, 64, DEV)
+    v = torch.full((600, 2, 64), x, device=DEV)
+    binding.cache_write(torch.zeros_like(v), v, _i32(range(600)), cache)
+    lse = torch.zeros(1, 2, device=DEV)
+    out = binding.cache_attend(torch.zeros(1, 2, 64, dtype=torch.bfloat16, device=DEV), _i32([0, 1]), _i32([600]), _i32(range(38)).view(1, -1), cache,
+                               max_q_len=1, max_seq_len=600, lse=lse)
+    # half a step of the code (at least 64 of them), half a step of bf16, and the sums
+    assert ((out.double() - x).abs() <= (2.0 ** -7 + 2.0 ** -8 + 2.0 ** -10) * x).all() and (lse - math.log(600)).abs().max() < 1e-4
