@@ -37,7 +37,7 @@ struct AttendArgs {
     float *lse;
 };
 
-constexpr float kAtNothing = -1e30f;         // m' of a row that has seen nothing yet (finite: -inf minus it is still -inf)
+constexpr float kAtNothing = -3.4028235e38f; // m' of a row that has seen nothing yet: no score is less (finite: -inf minus it is still -inf)
 constexpr float kAtSlack = 8.f;              // m' follows the maximum only where a weight would pass 2^8 (fp16 ends at 2^16)
 constexpr float kAtLowLog = -60.f, kAtHighLog = 20.f;      // log2(vs) for which l may have m' as its reference
 constexpr float kAtZeroLog = -200.f;         // log2(vs) of a block of scale 0

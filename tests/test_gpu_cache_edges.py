@@ -142,3 +142,25 @@ def test_written_values_of_any_size_are_read_back(x):
                                max_q_len=1, max_seq_len=600, lse=lse)
     # half a step of the code (at least 64 of them), half a step of bf16, and the sums
     assert ((out.double() - x).abs() <= (2.0 ** -7 + 2.0 ** -8 + 2.0 ** -10) * x).all() and (lse - math.log(600)).abs().max() < 1e-4
+
+
+# ---- attention: scores far below zero --------------------------------------------------------------------------------
+
+@pytest.mark.usefixtures("bounds")
+@pytest.mark.parametrize("new", [[1], [6], [150]])
+def test_attend_scores_of_any_size_that_fp32_holds(new):
+    # equal scores of -2^103 and -2^120: a row that sees them sees something
+    q, off, L, tables, cache = _batch(new, [200], 4, 2, 128, 16, 6)
+    cache.k.fill_(64)
+    cache.v_scale.fill_(2.0 ** -4)
+    for size in (60, 77):
+        q.fill_(2.0 ** size)
+        cache.k_scale.fill_(2.0 ** 30)
+        lse = torch.zeros(q.shape[:2], device=DEV)
+        out = binding.cache_attend(q, off, L, tables, cache, max_q_len=max(new), max_seq_len=200, scale=-1.0, causal=False, lse=lse)
+        n = new[0]
+        ids = tables[0, :13].long()
+        mean = (cache.v[ids].double().transpose(0, 1).reshape(2, -1, 128)[:, :200] / 16).mean(1).repeat_interleave(2, 0)
+        # (a mean of 200 codes of equal weight: the output's rounding and the sums)
+        assert ((out[:n].double() - mean).abs() <= 2.0 ** -8 * mean.abs() + 2.0 ** -10 * 8).all()
+        assert ((lse[:n].double() / -(2.0 ** (size + 43))) - 1).abs().max() < 2.0 ** -20
