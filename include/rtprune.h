@@ -357,7 +357,8 @@ typedef struct {
  *   block_tables  DEVICE int32 [batch] rows, table_stride apart, of max_pages entries: those of new pages are written, all others kept
  * Outputs, DEVICE int32: slot_map [total_rows] (-1 in rows of no request), positions [total_rows] (-1 there; may be NULL),
  * seq_lens [batch] (cached and new tokens), state [2] = {*free_head + pages handed out, RTPRUNE_DEV_* bits}.
- * `state` must not be `free_head`.  Where the free list or a table row is too short, the tokens
+ * No output may overlap an input or another output (RTPRUNE_ERR_INVALID_ARG): the next step's context_lens and free_head are copies of this
+ * one's seq_lens and state[0], or the two alternate.  Where the free list or a table row is too short, the tokens
  * without a page get slot -1 (their table entry -1) and RTPRUNE_DEV_NO_PAGES is set; a request whose lengths are outside the contract gets
  * no pages, slots -1 and length 0, and RTPRUNE_DEV_BAD_OFFSETS is set.  One kernel.
  */

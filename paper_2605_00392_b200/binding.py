@@ -463,7 +463,8 @@ def map_pages(offsets: torch.Tensor, block_tables: torch.Tensor, free_pages: tor
               position_base: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """rtprune_page_map: hands pages of the free list to a ragged batch's new tokens, on the device.  `offsets` [batch + 1] and
     `token_index` are a run's out_offsets and kept_idx; `block_tables` [batch, max_pages] gets the new pages' entries; `out` is a
-    PageMap (or four tensors like it), of as many rows as `out.slot_map` has."""
+    PageMap (or four tensors like it), of as many rows as `out.slot_map` has.  Outputs share no memory with inputs: for the next step, copy
+    `out.seq_lens` and `out.state[:1]` into the tensors that are its context_lens and free_head, or use two PageMaps in turn."""
     slots, positions, lens, state = out
     dev, batch, rows = offsets.get_device(), offsets.numel() - 1, slots.numel()
     if dev < 0 or batch < 0:

@@ -127,6 +127,24 @@ page_map_kernel(const int32_t *__restrict__ offsets, const int32_t *__restrict__
     }
 }
 
+// Words of memory that a call reads or writes: `rows` runs of `words`, `stride` apart.
+struct Words {
+    const int32_t *p;
+    int64_t words, rows = 1, stride = 0;
+};
+// Whether two pieces of memory share a byte (b: one run).
+static bool overlap(const Words &a, const Words &b)
+{
+    if (!a.p || !b.p || a.words <= 0 || b.words <= 0 || a.rows <= 0) return false;
+    const int64_t from = (int64_t)((intptr_t)b.p - (intptr_t)a.p), to = from + b.words * 4;      // b, in bytes from a's first
+    const int64_t pitch = a.stride * 4, len = a.words * 4;
+    if (to <= 0 || from >= (a.rows - 1) * pitch + len) return false;
+    if (a.rows == 1) return true;
+    // the run that b begins in (or the first), and the next
+    const int64_t row = std::max<int64_t>(0, from / pitch);
+    return from < row * pitch + len || (row + 1 < a.rows && to > (row + 1) * pitch);
+}
+
 // ---- codes and scales -----------------------------------------------------------------------------------------------
 //
 // A page is one block of tokens: each kv head of it has one scale for its keys and one for its values, the smallest
@@ -340,7 +358,15 @@ extern "C" rtprune_status_t rtprune_page_map(void *cuda_stream, const int32_t *o
     if (!offsets || !free_head || !seq_lens || !state || (!free_pages && n_free) || (!block_tables && max_pages) ||
         (!slot_map && total_rows))
         return RTPRUNE_ERR_INVALID_ARG;
-    if (state == free_head) return RTPRUNE_ERR_INVALID_ARG;      // every CTA reads the head, one writes the state
+    // every CTA reads the lengths, the lists and the head, whichever wrote its part of the outputs before
+    const Words in[] = {{offsets, batch + 1}, {context_lens, batch}, {position_base, batch}, {token_index, total_rows}, {free_pages, n_free}, {free_head, 1}};
+    const Words out[] = {{block_tables, max_pages, batch, table_stride}, {slot_map, total_rows}, {positions, total_rows}, {seq_lens, batch}, {state, 2}};
+    for (int o = 0; o < 5; ++o) {
+        for (const Words &i : in)
+            if (overlap(out[o], i)) return RTPRUNE_ERR_INVALID_ARG;
+        for (int other = o + 1; other < 5; ++other)
+            if (overlap(out[o], out[other])) return RTPRUNE_ERR_INVALID_ARG;
+    }
     int shift = 4;
     while ((1 << shift) < page_size) ++shift;
     const int64_t per_cta = kPmThreads * kPmRows;

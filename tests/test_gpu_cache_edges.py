@@ -164,3 +164,72 @@ def test_attend_scores_of_any_size_that_fp32_holds(new):
         # (a mean of 200 codes of equal weight: the output's rounding and the sums)
         assert ((out[:n].double() - mean).abs() <= 2.0 ** -8 * mean.abs() + 2.0 ** -10 * 8).all()
         assert ((lse[:n].double() / -(2.0 ** (size + 43))) - 1).abs().max() < 2.0 ** -20
+
+
+# ---- page tables: memory beside the outputs ----------------------------------------------------------------------------
+
+def test_page_map_in_one_piece_of_memory():
+    """All of a call's arrays back to back, and the lengths in the columns behind a table's rows: nothing overlaps, nothing is refused."""
+    new, ctx, page = [5, 0, 20], [3, 16, 31], 16
+    off, rows, batch = [0, 5, 5, 25], 27, 3
+    arena = torch.full((4096,), -9, dtype=torch.int32, device=DEV)
+    at = 0
+
+    def take(n, values=None):
+        nonlocal at
+        t = arena[at:at + n]
+        at += n
+        if values is not None:
+            t.copy_(_i32(values))
+        return t
+
+    o, c, free, head = take(4, off), take(3, ctx), take(6, [9, 8, 7, 6, 5, 4]), take(1, [1])
+    slots, pos, lens, state = take(27), take(27), take(3), take(2)
+    take(-at % 4)                                                          # (16-byte stores of rows need it)
+    wide = take(3 * 8).view(3, 8)
+    tables = wide[:, :5]
+    tables.copy_(_i32([[0, -1, -1, -1, -1], [1, -1, -1, -1, -1], [2, 3, -1, -1, -1]]))
+    base = wide[1, 5:]                                                     # a row's unused columns
+    base.copy_(_i32([100, 200, 300]))
+    want = ref.page_map(off, ctx, rows, page, [9, 8, 7, 6, 5, 4], 1, tables.cpu().numpy(), None, [100, 200, 300])
+    binding.map_pages(o, tables, free, head, (slots, pos, lens, state), page_size=page, context_lens=c, position_base=base)
+    for got, w in zip((tables, slots, pos, lens), want):
+        assert got.tolist() == w.tolist()
+    assert state.tolist() == [want[4], 0] and base.tolist() == [100, 200, 300] and (arena[at:] == -9).all()
+
+
+def test_page_map_refuses_its_own_lengths_as_contexts():
+    # the decode loop that hands one step's lengths to the next in place
+    m = binding.PageMap.allocate(3, 3, DEV)
+    m.seq_lens.fill_(15)
+    t, off, free = torch.full((3, 4), 1, dtype=torch.int32, device=DEV), _i32([0, 1, 2, 3]), _i32([5, 6, 7, 8])
+    for bad in (dict(context_lens=m.seq_lens), dict(position_base=m.seq_lens), dict(token_index=m.positions)):
+        with pytest.raises(binding.RtpruneError):
+            binding.map_pages(off, t, free, _i32([0]), m, page_size=16, **bad)
+    with pytest.raises(binding.RtpruneError):
+        binding.map_pages(off, t, free, m.state[1:], m, page_size=16)
+    assert m.seq_lens.tolist() == [15] * 3
+
+
+@pytest.mark.parametrize("page,batch", [(16, 3), (64, 700)])
+def test_page_map_decode_loop_with_two_maps_in_turn(page, batch):
+    """Tokens one by one, the lengths of one map the contexts of the other: every token has a slot of its own, in order."""
+    maps = [binding.PageMap.allocate(batch, batch, DEV) for _ in range(2)]
+    off = torch.arange(batch + 1, dtype=torch.int32, device=DEV)
+    tables = torch.full((batch, 5), -1, dtype=torch.int32, device=DEV)
+    free = torch.arange(5 * batch, dtype=torch.int32, device=DEV).flip(0).contiguous()
+    maps[1].seq_lens.copy_(torch.arange(batch, device=DEV) % 3)
+    maps[1].state.zero_()
+    taken = sum(1 for i in range(batch) if i % 3)                          # pages for the tokens that are there
+    tables[maps[1].seq_lens > 0, 0] = free[:taken]
+    maps[1].state[0] = taken
+    seen = set()
+    for t in range(2 * page + 3):
+        m, before = maps[t % 2], maps[(t + 1) % 2]
+        binding.map_pages(off, tables, free, before.state[:1], m, page_size=page, context_lens=before.seq_lens)
+        x = before.seq_lens.long()
+        assert m.state[1] == 0 and torch.equal(m.seq_lens, before.seq_lens + 1) and torch.equal(m.positions.long(), x)
+        assert torch.equal(m.slot_map.long(), tables.long()[torch.arange(batch, device=DEV), x // page] * page + x % page)
+        slots = m.slot_map.tolist()
+        assert not seen & set(slots) and len(set(slots)) == batch
+        seen |= set(slots)
