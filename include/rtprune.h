@@ -360,7 +360,7 @@ typedef struct {
  * No output may overlap an input or another output (RTPRUNE_ERR_INVALID_ARG): the next step's context_lens and free_head are copies of this
  * one's seq_lens and state[0], or the two alternate.  Where the free list or a table row is too short, the tokens
  * without a page get slot -1 (their table entry -1) and RTPRUNE_DEV_NO_PAGES is set; a request whose lengths are outside the contract gets
- * no pages, slots -1 and length 0, and RTPRUNE_DEV_BAD_OFFSETS is set.  One kernel.
+ * no pages, slots -1 and length 0, and RTPRUNE_DEV_BAD_OFFSETS is set.  One kernel.  With batch = 0 (and no rows) nothing is launched or written.
  */
 rtprune_status_t rtprune_page_map(void *cuda_stream, const int32_t *offsets, const int32_t *context_lens, int32_t batch,
                                   int64_t total_rows, const int32_t *token_index, const int32_t *position_base,

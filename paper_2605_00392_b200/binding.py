@@ -478,6 +478,10 @@ def map_pages(offsets: torch.Tensor, block_tables: torch.Tensor, free_pages: tor
                table, table_stride, pages, _int32(slots, 0, dev, "slot_map"),
                None if positions is None else _int32(positions, rows, dev, "positions"), _int32(lens, batch, dev, "seq_lens"),
                _int32(state, 2, dev, "state"))
+    if batch == 0:                             # the library writes nothing for no requests
+        with torch.cuda.stream(stream):
+            state[:1].copy_(free_head[:1])
+            state[1:2].zero_()
 
 
 def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor,

@@ -233,3 +233,16 @@ def test_page_map_decode_loop_with_two_maps_in_turn(page, batch):
         slots = m.slot_map.tolist()
         assert not seen & set(slots) and len(set(slots)) == batch
         seen |= set(slots)
+
+
+def test_page_map_of_no_requests():
+    # the free list goes on from where it was
+    m = binding.PageMap.allocate(0, 0, DEV)
+    m.state.fill_(77)
+    side = torch.cuda.Stream()
+    for stream in (None, side):
+        side.wait_stream(torch.cuda.current_stream())
+        binding.map_pages(_i32([0]), torch.empty(0, 4, dtype=torch.int32, device=DEV), _i32([5, 6]), _i32([1]), m, page_size=16, stream=stream)
+        torch.cuda.current_stream().wait_stream(side)
+        assert m.state.tolist() == [1, 0]
+        m.state.fill_(77)
