@@ -356,10 +356,12 @@ typedef struct {
  *   free_pages    DEVICE int32 [n_free] page ids; free_head DEVICE int32 [1]
  *   block_tables  DEVICE int32 [batch] rows, table_stride apart, of max_pages entries: those of new pages are written, all others kept
  * Outputs, DEVICE int32: slot_map [total_rows] (-1 in rows of no request), positions [total_rows] (-1 there; may be NULL),
- * seq_lens [batch] (cached and new tokens), state [2] = {*free_head + pages handed out, RTPRUNE_DEV_* bits}.
+ * seq_lens [batch] (cached and new tokens), state [2] = {*free_head + pages that the requests need, n_free at most, RTPRUNE_DEV_* bits}.
  * No output may overlap an input or another output (RTPRUNE_ERR_INVALID_ARG): the next step's context_lens and free_head are copies of this
  * one's seq_lens and state[0], or the two alternate.  Where the free list or a table row is too short, the tokens
- * without a page get slot -1 (their table entry -1) and RTPRUNE_DEV_NO_PAGES is set; a request whose lengths are outside the contract gets
+ * without a page get slot -1 (their table entry -1) and RTPRUNE_DEV_NO_PAGES is set.  Pages for entries that a row does not have are counted in
+ * state[0] all the same and are in no table; nothing is lost where the call is repeated from the old head (with longer rows or a longer list):
+ * it hands out the same pages again.  A request whose lengths are outside the contract gets
  * no pages, slots -1 and length 0, and RTPRUNE_DEV_BAD_OFFSETS is set.  One kernel.  With batch = 0 (and no rows) nothing is launched or written.
  */
 rtprune_status_t rtprune_page_map(void *cuda_stream, const int32_t *offsets, const int32_t *context_lens, int32_t batch,

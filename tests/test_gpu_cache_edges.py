@@ -246,3 +246,19 @@ def test_page_map_of_no_requests():
         torch.cuda.current_stream().wait_stream(side)
         assert m.state.tolist() == [1, 0]
         m.state.fill_(77)
+
+
+def test_page_map_again_after_too_short_a_row():
+    """RTPRUNE_DEV_NO_PAGES: the call repeated from the old head, with rows that are wide enough, is as if the first had not been."""
+    off, ctx, free = _i32([0, 40, 45]), _i32([3, 0]), _i32([9, 8, 7, 6])
+    wide = torch.full((2, 4), -1, dtype=torch.int32, device=DEV)
+    wide[0, 0] = 2
+    one, m = wide.clone(), binding.PageMap.allocate(45, 2, DEV)
+    binding.map_pages(off, wide[:, :2], free, _i32([0]), m, page_size=16, context_lens=ctx)
+    # the second request's page comes behind both of the first's, of which its row could take one
+    assert m.state.tolist() == [3, binding.DEV_NO_PAGES] and wide.tolist() == [[2, 9, -1, -1], [7, -1, -1, -1]]
+    assert (m.slot_map[29:40] == -1).all() and m.slot_map[40] == 7 * 16
+    binding.map_pages(off, wide, free, _i32([0]), m, page_size=16, context_lens=ctx)
+    once = binding.PageMap.allocate(45, 2, DEV)
+    binding.map_pages(off, one, free, _i32([0]), once, page_size=16, context_lens=ctx)
+    assert torch.equal(wide, one) and all(torch.equal(a, b) for a, b in zip(m, once)) and m.state.tolist() == [3, 0]
