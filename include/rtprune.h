@@ -414,6 +414,7 @@ rtprune_status_t rtprune_cache_write(void *cuda_stream, rtprune_dtype_t dtype, c
  * scale NaN, or whose query is not finite, gives NaN (an infinite query may also give 0 or the values of its largest scores), and so does a row of a request that sees an entry of its table outside the cache or whose
  * seq_lens is outside 0 .. max_seq_len.  A request of more than max_q_len rows is passed over.  Values agree with those formulas in 64 bits to
  * the rounding of bf16, whatever the scales (0, or 2^-126 to 2^121, beside one another; never negative); the softmax and all sums are fp32.  What a row's result is does not depend on the call's timing.
+ * Waits inside the kernels are bounded by the call's sizes; should one give up all the same, the rows that it holds up are NaN, none is left unwritten.
  *
  *   q            DEVICE bf16 [rows] rows of q_heads heads of head_dim, 16-byte aligned, row stride in elements, a multiple of 8
  *   offsets      DEVICE int32 [batch+1], seq_lens DEVICE int32 [batch]; batch <= 65535
@@ -433,6 +434,13 @@ rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *q, int64_t 
                                       int64_t max_seq_len, const int32_t *block_tables, int64_t table_stride, int32_t max_pages,
                                       const rtprune_cache_t *cache, float scale, int32_t causal, void *out, float *lse,
                                       void *workspace, size_t workspace_bytes);
+
+/* Test aid: rtprune_cache_attend with waits that give up at once (NaN in every row of a request). */
+rtprune_status_t rtprune_test_cache_attend_expired(void *cuda_stream, const void *q, int64_t q_stride, int64_t rows, int32_t q_heads,
+                                                   const int32_t *offsets, const int32_t *seq_lens, int32_t batch, int32_t max_q_len,
+                                                   int64_t max_seq_len, const int32_t *block_tables, int64_t table_stride, int32_t max_pages,
+                                                   const rtprune_cache_t *cache, float scale, int32_t causal, void *out, float *lse,
+                                                   void *workspace, size_t workspace_bytes);
 
 /*
  * Test aid: makes the library's bounded device-side waits run out without any fault.  Launches one small

@@ -133,13 +133,14 @@ extern "C" rtprune_status_t rtprune_cache_attend_workspace(int32_t batch, int32_
     return RTPRUNE_OK;
 }
 
-extern "C" rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *q, int64_t q_stride, int64_t rows, int32_t q_heads,
-                                                 const int32_t *offsets, const int32_t *seq_lens, int32_t batch, int32_t max_q_len,
-                                                 int64_t max_seq_len, const int32_t *block_tables, int64_t table_stride,
-                                                 int32_t max_pages, const rtprune_cache_t *cache, float scale, int32_t causal,
-                                                 void *out, float *lse, void *workspace, size_t workspace_bytes)
+namespace rtp {
+
+// rtprune_cache_attend; expired: waits that give up at once.
+static rtprune_status_t cache_attend(void *cuda_stream, const void *q, int64_t q_stride, int64_t rows, int32_t q_heads, const int32_t *offsets,
+                                     const int32_t *seq_lens, int32_t batch, int32_t max_q_len, int64_t max_seq_len,
+                                     const int32_t *block_tables, int64_t table_stride, int32_t max_pages, const rtprune_cache_t *cache,
+                                     float scale, int32_t causal, void *out, float *lse, void *workspace, size_t workspace_bytes, bool expired)
 {
-    using namespace rtp;
     CacheView c;
     rtprune_status_t status;
     if (rows < 0 || batch < 0 || max_q_len < 0 || max_seq_len < 0 || q_heads <= 0 || max_pages < 0 || table_stride < max_pages ||
@@ -160,11 +161,13 @@ extern "C" rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *
     if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255u)) return RTPRUNE_ERR_WORKSPACE;
     AttendArgs a = {(const __nv_bfloat16 *)q, q_stride, offsets, seq_lens, block_tables, table_stride, batch, (int)rows, q_heads,
                     q_heads / c.kv_heads, max_q_len, (int)max_seq_len, max_pages, c, scale * 1.4426950408889634f, causal ? 1 : 0,
-                    (__nv_bfloat16 *)out, lse};
+                    (__nv_bfloat16 *)out, lse, 0};
     if (few_rows(batch, max_q_len, c.kv_heads, a.group)) {
         // a tile's first row has 26 bits of a word, and a CTA's blocks (of half a 148th of the line, and fewer) an int
         const int64_t most = std::min<int64_t>(max_q_len, rows) * a.group, tiles = (most + 7) / 8 * batch * c.kv_heads;
         if (most >= 1 << 26 || tiles * (max_seq_len / kArBlock + 1) / 64 > INT32_MAX) return RTPRUNE_ERR_UNSUPPORTED;
+        // a wait lasts as long as the fetching warp looks for the next request that has rows, at most
+        if (!expired) a.polls = ptx::kSpinLimit + 512u * (uint32_t)batch;
         uint8_t *ws = (uint8_t *)workspace;
         cudaStream_t st = (cudaStream_t)cuda_stream;
         // tiles of 8 rows where a request has no more: 64 steps 37 us against 51 with 16, 16 long ones of 4 heads 116 against 153 (at 32 rows of
@@ -176,8 +179,36 @@ extern "C" rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *
         return cudaGetLastError() == cudaSuccess ? RTPRUNE_OK : RTPRUNE_ERR_CUDA;
     }
     if (tile_row_blocks(a) * batch * c.kv_heads > INT32_MAX / 2) return RTPRUNE_ERR_UNSUPPORTED;
+    // waits last as long as the items that are ahead, at most (five of them, some 7000 cycles a block each), and the search for the next one (a
+    // thousand cycles for 32 numbers); a poll is 20 cycles or more
+    if (!expired)
+        a.polls = ptx::kSpinLimit + 4096u * (uint32_t)std::min<int64_t>(max_seq_len / kTlBlock + 1, 1 << 19) +
+                  16u * (uint32_t)(tile_row_blocks(a) * batch * c.kv_heads / std::max(device_sms(), 1) + 1);
     const cudaError_t e = c.dim == 128 ? launch_tiles<128>(a, (cudaStream_t)cuda_stream) : launch_tiles<64>(a, (cudaStream_t)cuda_stream);
     if (e != cudaSuccess)
         return RTPRUNE_ERR_CUDA;
     return cudaGetLastError() == cudaSuccess ? RTPRUNE_OK : RTPRUNE_ERR_CUDA;
+}
+
+}  // namespace rtp
+
+extern "C" rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *q, int64_t q_stride, int64_t rows, int32_t q_heads,
+                                                 const int32_t *offsets, const int32_t *seq_lens, int32_t batch, int32_t max_q_len,
+                                                 int64_t max_seq_len, const int32_t *block_tables, int64_t table_stride,
+                                                 int32_t max_pages, const rtprune_cache_t *cache, float scale, int32_t causal,
+                                                 void *out, float *lse, void *workspace, size_t workspace_bytes)
+{
+    return rtp::cache_attend(cuda_stream, q, q_stride, rows, q_heads, offsets, seq_lens, batch, max_q_len, max_seq_len, block_tables, table_stride,
+                             max_pages, cache, scale, causal, out, lse, workspace, workspace_bytes, false);
+}
+
+extern "C" rtprune_status_t rtprune_test_cache_attend_expired(void *cuda_stream, const void *q, int64_t q_stride, int64_t rows, int32_t q_heads,
+                                                              const int32_t *offsets, const int32_t *seq_lens, int32_t batch,
+                                                              int32_t max_q_len, int64_t max_seq_len, const int32_t *block_tables,
+                                                              int64_t table_stride, int32_t max_pages, const rtprune_cache_t *cache,
+                                                              float scale, int32_t causal, void *out, float *lse, void *workspace,
+                                                              size_t workspace_bytes)
+{
+    return rtp::cache_attend(cuda_stream, q, q_stride, rows, q_heads, offsets, seq_lens, batch, max_q_len, max_seq_len, block_tables, table_stride,
+                             max_pages, cache, scale, causal, out, lse, workspace, workspace_bytes, true);
 }

@@ -35,7 +35,14 @@ struct AttendArgs {
     int32_t causal;
     __nv_bfloat16 *out;
     float *lse;
+    uint32_t polls;                          // after which a wait gives up: the rows that hang on it, and those of the CTA's later work, come out NaN
 };
+
+// Bounded wait of a whole warp: no lane goes on as if what the others gave up on were there.
+__device__ inline bool attend_wait(const AttendArgs &a, uint64_t *bar, uint32_t parity)
+{
+    return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, a.polls));
+}
 
 constexpr float kAtNothing = -3.4028235e38f; // m' of a row that has seen nothing yet: no score is less (finite: -inf minus it is still -inf)
 constexpr float kAtSlack = 8.f;              // m' follows the maximum only where a weight would pass 2^8 (fp16 ends at 2^16)

@@ -190,7 +190,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
     __shared__ float row_factor[kArRows];
     __shared__ float2 row_ml[kArWarps][R];
     __shared__ float row_ref[kArWarps][R];           // r of a warp's rows once they have one; infinity before (it is m' then)
-    __shared__ float4 scales[S::kStages][kArWarps];  // ks, log2 vs, 1 / vs of each warp's 16 tokens; w: 1 from the tile's first wide one on
+    __shared__ float4 scales[S::kStages][kArWarps];  // ks, log2 vs, 1 / vs of each warp's 16 tokens; w: infinity from the tile's first wide one on, else 0
     __shared__ uint64_t full[S::kStages], empty[S::kStages];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     const uint32_t ring = ptx::smem_u32(sm), frag = ring + S::kRing, scales_u32 = ptx::smem_u32(scales);
@@ -235,7 +235,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
                 const uint32_t s = n % S::kStages, turn = n / S::kStages, to = ring + s * 2 * S::kBytes;
                 const float ks = block < 0 ? nan : __ldg(a.c.k_scale + block), vs = block < 0 ? nan : __ldg(a.c.v_scale + block);
                 bool ok = true;
-                if (turn > 0) ok = ptx::mbar_wait(&empty[s], (turn - 1) & 1);
+                if (turn > 0) ok = ptx::mbar_wait(&empty[s], (turn - 1) & 1, a.polls);
                 if (!__all_sync(0xffffffffu, ok)) break;
                 const int64_t from = ((int64_t)max(block, 0) * a.c.page_size + slot) * D;
 #pragma unroll
@@ -253,7 +253,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
                 ptx::cp_async_arrive(&full[s]);
                 float lv, inv;
                 wide = value_scale(vs, lv, inv) || (wide && !fresh);
-                if ((lane & 7) == 0) scales[s][lane >> 3] = make_float4(ks, lv, inv, wide ? 1.f : 0.f);
+                if ((lane & 7) == 0) scales[s][lane >> 3] = make_float4(ks, lv, inv, wide ? INFINITY : 0.f);
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&full[s]);
                 ++n;
@@ -262,8 +262,8 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
             slot = next_slot;
             fresh = next_fresh;
         }
-        ptx::cp_async_commit();
-        ptx::cp_async_wait<0>();                     // no copy is left on its way into memory that this CTA gives back
+        // no copy, nor its arrival, is left on its way into memory that this CTA gives back
+        for (uint32_t c = n > S::kStages ? n - S::kStages : 0; c < n; ++c) ptx::mbar_wait(&full[c % S::kStages], c / S::kStages & 1);
         return;
     }
 
@@ -369,9 +369,11 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
         uint32_t stage = n % S::kStages, parity = n / S::kStages & 1;
 #pragma unroll 1
         for (int b = 0; b < steps; ++b, t0 += kArBlock) {
-            if (!dead && !ptx::mbar_wait(&full[stage], parity)) dead = true;
+            // (lane by lane: nothing below branches on it, and what a lane reads of a step that is not there are codes and scales all the same)
+            if (!dead && !ptx::mbar_wait(&full[stage], parity, a.polls)) dead = true;
+            __syncwarp();
             const uint32_t kt = ring + stage * 2 * S::kBytes + warp * 16 * D, vt = kt + S::kBytes;
-            if (t0 < hi_end && !dead) {
+            if (t0 < hi_end) {
                 const float4 sc = lds_f4(scales_u32 + (stage * kArWarps + warp) * 16);
                 if constexpr (R == 8) {
                     // ---- scores of tokens t0 + g (s[0], s[1]) and 8 more (s[2], s[3]) for rows 2c, 2c + 1
@@ -390,49 +392,52 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
                     }
                     // ---- weights
                     const float k0 = f0 * sc.x, k1 = f1 * sc.x;
-                    if (t0 + 16 > lo_end || sc.w != 0.f) {
-                        // tokens that a row does not see, or a reference of its own for l, from here to the tile's end: the largest s and s'
-                        // are taken every time
-                        bool seen[4];
-                        float top_s[2], top[2], r[2];
+                    float w[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            s[e] *= e & 1 ? k1 : k0;
-                            seen[e] = t0 + g + 8 * (e >> 1) < end[e & 1];
-                        }
+                    for (int e = 0; e < 4; ++e) w[e] = fmaf(s[e], e & 1 ? k1 : k0, sc.y);
+                    const float top0 = fmaxf(w[0], w[2]), top1 = fmaxf(w[1], w[3]);
+                    bool careful = t0 + 16 > lo_end;
+                    if (__any_sync(0xffffffffu, careful || fmaxf(fmaxf(top0 - m[0], top1 - m[1]), sc.w) > kAtSlack)) {
+                        careful = careful || __any_sync(0xffffffffu, sc.w != 0.f);
+                        if (careful) {
+                            // tokens that a row does not see, or a reference of its own for l, from here to the tile's end: the largest s and
+                            // s' are taken every time
+                            bool seen[4];
+                            float top_s[2], top[2], r[2];
 #pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            top_s[x] = fmaxf(seen[x] ? s[x] : -INFINITY, seen[2 + x] ? s[2 + x] : -INFINITY);
-#pragma unroll
-                            for (int o = 4; o < 32; o <<= 1) top_s[x] = fmaxf(top_s[x], __shfl_xor_sync(0xffffffffu, top_s[x], o));
-                            r[x] = row_ref[warp][mine[x]];
-                            if (r[x] == INFINITY) r[x] = m[x];
-                            top[x] = fmaxf(m[x], top_s[x] + sc.y);
-                            const float to = fmaxf(r[x], top_s[x]), k = ex2(m[x] - top[x]);
-                            l[x] *= ex2(r[x] - to);
-                            m[x] = top[x];
-                            r[x] = to;
-#pragma unroll
-                            for (int j = 0; j < S::kNt; ++j) {
-                                acc[j][x] *= k;
-                                acc[j][x + 2] *= k;
+                            for (int e = 0; e < 4; ++e) {
+                                s[e] *= e & 1 ? k1 : k0;
+                                seen[e] = t0 + g + 8 * (e >> 1) < end[e & 1];
                             }
-                        }
-                        __syncwarp();
 #pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            if (g == 0) row_ref[warp][mine[x]] = r[x];
-                            const float gap = m[x] - r[x], lv = weight_log(sc.y, gap);
-                            s[x] = seen[x] ? ex2(s[x] + lv - m[x]) : 0.f;
-                            s[2 + x] = seen[2 + x] ? ex2(s[2 + x] + lv - m[x]) : 0.f;
-                            if (seen[x] || seen[2 + x]) l[x] = fmaf(s[x] + s[2 + x], ex2(gap - lv), l[x]);
-                        }
-                        __syncwarp();
-                    } else {
+                            for (int x = 0; x < 2; ++x) {
+                                top_s[x] = fmaxf(seen[x] ? s[x] : -INFINITY, seen[2 + x] ? s[2 + x] : -INFINITY);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[e] = fmaf(s[e], e & 1 ? k1 : k0, sc.y);
-                        const float top0 = fmaxf(s[0], s[2]), top1 = fmaxf(s[1], s[3]);
-                        if (__any_sync(0xffffffffu, fmaxf(top0 - m[0], top1 - m[1]) > kAtSlack)) {
+                                for (int o = 4; o < 32; o <<= 1) top_s[x] = fmaxf(top_s[x], __shfl_xor_sync(0xffffffffu, top_s[x], o));
+                                r[x] = row_ref[warp][mine[x]];
+                                if (r[x] == INFINITY) r[x] = m[x];
+                                top[x] = fmaxf(m[x], top_s[x] + sc.y);
+                                const float to = fmaxf(r[x], top_s[x]), k = ex2(m[x] - top[x]);
+                                l[x] *= ex2(r[x] - to);
+                                m[x] = top[x];
+                                r[x] = to;
+#pragma unroll
+                                for (int j = 0; j < S::kNt; ++j) {
+                                    acc[j][x] *= k;
+                                    acc[j][x + 2] *= k;
+                                }
+                            }
+                            __syncwarp();
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                if (g == 0) row_ref[warp][mine[x]] = r[x];
+                                const float gap = m[x] - r[x], lv = weight_log(sc.y, gap);
+                                s[x] = seen[x] ? ex2(s[x] + lv - m[x]) : 0.f;
+                                s[2 + x] = seen[2 + x] ? ex2(s[2 + x] + lv - m[x]) : 0.f;
+                                if (seen[x] || seen[2 + x]) l[x] = fmaf(s[x] + s[2 + x], ex2(gap - lv), l[x]);
+                            }
+                            __syncwarp();
+                        } else {
                             float n0 = top0, n1 = top1;
 #pragma unroll
                             for (int o = 4; o < 32; o <<= 1) {
@@ -454,8 +459,10 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
                                 acc[j][3] *= c1;
                             }
                         }
+                    }
+                    if (!careful) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[e] = ex2(s[e] - m[e & 1]);
+                        for (int e = 0; e < 4; ++e) s[e] = ex2(w[e] - m[e & 1]);
                         l[0] = fmaf(s[0] + s[2], sc.z, l[0]);
                         l[1] = fmaf(s[1] + s[3], sc.z, l[1]);
                     }
@@ -509,50 +516,52 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
                     }
                     // ---- weights
                     const float k0 = f0 * sc.x, k1 = f1 * sc.x;
-                    if (t0 + 16 > lo_end || sc.w != 0.f) {
-                        // tokens that a row does not see, or a reference of its own for l, from here to the tile's end: the largest s and s'
-                        // are taken every time
+                    float w[2][4];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {        // row g + 8 h: its scores are s[0][2h], s[0][2h + 1], s[1][2h], s[1][2h + 1]
-                            float top_s = -INFINITY;
+                    for (int x = 0; x < 2; ++x)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                float &x = s[e >> 1][2 * h + (e & 1)];
-                                x *= h ? k1 : k0;
-                                if (t0 + 8 * (e >> 1) + 2 * c + (e & 1) < end[h]) top_s = fmaxf(top_s, x);
+                        for (int e = 0; e < 4; ++e) w[x][e] = fmaf(s[x][e], e < 2 ? k0 : k1, sc.y);
+                    const float top0 = fmaxf(fmaxf(w[0][0], w[0][1]), fmaxf(w[1][0], w[1][1]));
+                    const float top1 = fmaxf(fmaxf(w[0][2], w[0][3]), fmaxf(w[1][2], w[1][3]));
+                    bool careful = t0 + 16 > lo_end;
+                    if (__any_sync(0xffffffffu, careful || fmaxf(fmaxf(top0 - m[0], top1 - m[1]), sc.w) > kAtSlack)) {
+                        careful = careful || __any_sync(0xffffffffu, sc.w != 0.f);
+                        if (careful) {
+                            // (as with 8 rows)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {        // row g + 8 h: its scores are s[0][2h], s[0][2h + 1], s[1][2h], s[1][2h + 1]
+                                float top_s = -INFINITY;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    float &x = s[e >> 1][2 * h + (e & 1)];
+                                    x *= h ? k1 : k0;
+                                    if (t0 + 8 * (e >> 1) + 2 * c + (e & 1) < end[h]) top_s = fmaxf(top_s, x);
+                                }
+                                top_s = fmaxf(top_s, __shfl_xor_sync(0xffffffffu, top_s, 1));
+                                top_s = fmaxf(top_s, __shfl_xor_sync(0xffffffffu, top_s, 2));
+                                float r = row_ref[warp][mine[h]];
+                                if (r == INFINITY) r = m[h];
+                                const float top = fmaxf(m[h], top_s + sc.y), to = fmaxf(r, top_s), k = ex2(m[h] - top);
+                                l[h] *= ex2(r - to);
+                                m[h] = top;
+#pragma unroll
+                                for (int j = 0; j < S::kNt; ++j) {
+                                    acc[j][2 * h] *= k;
+                                    acc[j][2 * h + 1] *= k;
+                                }
+                                __syncwarp();
+                                if (c == 0) row_ref[warp][mine[h]] = to;
+                                __syncwarp();
+                                const float gap = top - to, lv = weight_log(sc.y, gap), z = ex2(gap - lv);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    float &x = s[e >> 1][2 * h + (e & 1)];
+                                    const bool seen = t0 + 8 * (e >> 1) + 2 * c + (e & 1) < end[h];
+                                    x = seen ? ex2(x + lv - top) : 0.f;
+                                    if (seen) l[h] = fmaf(x, z, l[h]);
+                                }
                             }
-                            top_s = fmaxf(top_s, __shfl_xor_sync(0xffffffffu, top_s, 1));
-                            top_s = fmaxf(top_s, __shfl_xor_sync(0xffffffffu, top_s, 2));
-                            float r = row_ref[warp][mine[h]];
-                            if (r == INFINITY) r = m[h];
-                            const float top = fmaxf(m[h], top_s + sc.y), to = fmaxf(r, top_s), k = ex2(m[h] - top);
-                            l[h] *= ex2(r - to);
-                            m[h] = top;
-#pragma unroll
-                            for (int j = 0; j < S::kNt; ++j) {
-                                acc[j][2 * h] *= k;
-                                acc[j][2 * h + 1] *= k;
-                            }
-                            __syncwarp();
-                            if (c == 0) row_ref[warp][mine[h]] = to;
-                            __syncwarp();
-                            const float gap = top - to, lv = weight_log(sc.y, gap), z = ex2(gap - lv);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                float &x = s[e >> 1][2 * h + (e & 1)];
-                                const bool seen = t0 + 8 * (e >> 1) + 2 * c + (e & 1) < end[h];
-                                x = seen ? ex2(x + lv - top) : 0.f;
-                                if (seen) l[h] = fmaf(x, z, l[h]);
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int x = 0; x < 2; ++x)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) s[x][e] = fmaf(s[x][e], e < 2 ? k0 : k1, sc.y);
-                        const float top0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
-                        const float top1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
-                        if (__any_sync(0xffffffffu, fmaxf(top0 - m[0], top1 - m[1]) > kAtSlack)) {
+                        } else {
                             float n0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, 1)), n1 = fmaxf(top1, __shfl_xor_sync(0xffffffffu, top1, 1));
                             n0 = fmaxf(m[0], fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, 2)));
                             n1 = fmaxf(m[1], fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, 2)));
@@ -569,10 +578,12 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
                                 acc[j][3] *= c1;
                             }
                         }
+                    }
+                    if (!careful) {
 #pragma unroll
                         for (int x = 0; x < 2; ++x)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) s[x][e] = ex2(s[x][e] - m[e >> 1]);
+                            for (int e = 0; e < 4; ++e) s[x][e] = ex2(w[x][e] - m[e >> 1]);
                         l[0] = fmaf((s[0][0] + s[0][1]) + (s[1][0] + s[1][1]), sc.z, l[0]);
                         l[1] = fmaf((s[0][2] + s[0][3]) + (s[1][2] + s[1][3]), sc.z, l[1]);
                     }
@@ -611,7 +622,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
             }
         }
         n += steps;
-        if (dead) l[0] = l[1] = __uint_as_float(0x7fc00000u);
+        if (__any_sync(0xffffffffu, dead)) l[0] = l[1] = __uint_as_float(0x7fc00000u);
 
         // ---- the warps' sums, put together in their order: to a common m', then 2 + 2, then 1 + 1
 #pragma unroll

@@ -20,6 +20,8 @@
 // range, and the sums, which are needed anyway, show it with less work than a maximum (772 us against 805 for 37 requests of 512 rows
 // that see 8512 tokens).  A tile's rows behind the request's last (the next request's queries, or whatever shared memory held where a
 // token's heads do not divide 128) are computed like the others, but have no voice in how a warp goes on: a row's bits do not hang on them.
+// Every wait is bounded, and the lanes of a warp take its result together.  Where one gives up its warp leaves; those that wait for it give
+// up too, and the softmax's warps write NaN to the rows of the item in work and of all that the CTA would have taken behind it.
 // Bound by the tensor cores and, about as much, by the exponentials: 128 x 128 scores take 1024 cycles of either (16 exponentials a
 // cycle and SM; two products of 128^3 at 4096 multiply-adds).  It takes 2200: 1.07 PFLOP/s at 512 rows over 8512 tokens, 211 us for 8 causal
 // requests of 2783 tokens and 97 us for 64 of 300 to 375, 10 heads.  Keys that need no conversion would make that 15 % less, a softmax
@@ -53,6 +55,7 @@ template <int D> struct TlShape {
 // A CTA's piece of work.
 struct TlItem {
     int i, head, j0, row0, n, len;                   // i < 0: no more; j0: first of its tokens, in the request
+    int after;                                       // where the CTA's numbers go on
     int blocks[kTlTiles];                            // blocks of tokens that each tile sees any of
 };
 constexpr int kTlItems = 4;                          // pieces that the scheduler may be ahead by, about
@@ -70,17 +73,59 @@ struct TlShared {
     uint64_t q_full[kTlTiles], q_empty[kTlTiles], s_full[kTlTiles], p_full[kTlTiles], o_full[kTlTiles], o_empty[kTlTiles];
     uint64_t turn[kTlTiles], done;
     uint32_t tmem;
-    volatile int gave_up;
+    volatile int gave_up, after[kTlSoft / 32];       // after: of the item that a warp of the softmax has in work
 };
 
-// The k-th item, for a whole warp.  false: a wait gave up.
-__device__ inline bool tl_take(TlShared *sh, uint32_t k, TlItem &t)
+// The k-th item, for a whole warp.  false: a wait gave up, and t is nothing.
+__device__ inline bool tl_take(const AttendArgs &a, TlShared *sh, uint32_t k, TlItem &t)
 {
-    const bool ok = ptx::mbar_wait(&sh->item_full[k % kTlItems], k / kTlItems & 1);
+    if (!attend_wait(a, &sh->item_full[k % kTlItems], k / kTlItems & 1)) return false;
     t = sh->item[k % kTlItems];
     __syncwarp();
     if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&sh->item_empty[k % kTlItems]);
-    return __all_sync(0xffffffffu, ok);
+    return true;
+}
+
+// The CTA's next item that has rows, from its `at`-th number on, for a whole warp; i < 0: there is none.
+__device__ inline void tl_next(const AttendArgs &a, int row_blocks, int tile_tokens, int at, TlItem &t)
+{
+    const int lane = threadIdx.x & 31, per = a.batch * a.c.kv_heads, all = row_blocks * per;
+    auto number = [&](int round) { return round * (int)gridDim.x + (int)(round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x); };
+    const int rounds = (all + (int)gridDim.x - 1) / (int)gridDim.x;
+    // 32 of the numbers at a time, one per lane (bounds that are far above the requests' lengths leave most of them empty)
+#pragma unroll 1
+    for (; at < rounds; at += 32) {
+        const int mine = number(at + lane);
+        bool has = false;
+        if (at + lane < rounds && mine < all) {
+            // the last rows of every request first: with a causal mask they have the most to do
+            const int rest = mine % per;
+            t.i = rest / a.c.kv_heads;
+            t.head = rest - t.i * a.c.kv_heads;
+            t.j0 = (row_blocks - 1 - mine / per) * kTlTiles * tile_tokens;
+            has = attend_request(a, t.i, t.row0, t.n, t.len) && t.j0 < t.n;
+        }
+        const uint32_t found = __ballot_sync(0xffffffffu, has);
+        if (found) {
+            const int from = __ffs(found) - 1;
+            t.after = at + from + 1;
+            t.i = __shfl_sync(0xffffffffu, t.i, from);
+            t.head = __shfl_sync(0xffffffffu, t.head, from);
+            t.j0 = __shfl_sync(0xffffffffu, t.j0, from);
+            t.row0 = __shfl_sync(0xffffffffu, t.row0, from);
+            t.n = __shfl_sync(0xffffffffu, t.n, from);
+            t.len = __shfl_sync(0xffffffffu, t.len, from);
+#pragma unroll
+            for (int x = 0; x < kTlTiles; ++x) {
+                const int first = t.j0 + x * tile_tokens, last = min(first + tile_tokens, t.n) - 1;
+                const int end = first >= t.n || t.len < 0 ? 0 : a.causal ? t.len - t.n + 1 + last : t.len;
+                t.blocks[x] = (max(end, 0) + kTlBlock - 1) / kTlBlock;
+            }
+            return;
+        }
+    }
+    t.i = -1;
+    t.after = at;
 }
 
 __device__ inline void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
@@ -350,50 +395,15 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         if (warp == 15) {
             // ---------------- the work: items blockIdx.x, + gridDim.x, ... that have rows; their queries, as they are, in the operand's
             // layout already
-            const int per = a.batch * a.c.kv_heads, all = row_blocks * per;
-            auto number = [&](int round) { return round * (int)gridDim.x + (int)(round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x); };
-            const int rounds = (all + (int)gridDim.x - 1) / (int)gridDim.x;
             int at = 0;
             bool ok = true;
             uint32_t uses[kTlTiles] = {0, 0};
     #pragma unroll 1
             for (uint32_t k = 0; ok; ++k) {
                 TlItem t;
-                t.i = -1;
-                // 32 of the numbers at a time, one per lane (bounds that are far above the requests' lengths leave most of them empty)
-    #pragma unroll 1
-                for (; at < rounds; at += 32) {
-                    const int mine = number(at + lane);
-                    bool has = false;
-                    if (at + lane < rounds && mine < all) {
-                        // the last rows of every request first: with a causal mask they have the most to do
-                        const int rest = mine % per;
-                        t.i = rest / a.c.kv_heads;
-                        t.head = rest - t.i * a.c.kv_heads;
-                        t.j0 = (row_blocks - 1 - mine / per) * kTlTiles * tile_tokens;
-                        has = attend_request(a, t.i, t.row0, t.n, t.len) && t.j0 < t.n;
-                    }
-                    const uint32_t found = __ballot_sync(0xffffffffu, has);
-                    if (found) {
-                        const int from = __ffs(found) - 1;
-                        at += from + 1;
-                        t.i = __shfl_sync(0xffffffffu, t.i, from);
-                        t.head = __shfl_sync(0xffffffffu, t.head, from);
-                        t.j0 = __shfl_sync(0xffffffffu, t.j0, from);
-                        t.row0 = __shfl_sync(0xffffffffu, t.row0, from);
-                        t.n = __shfl_sync(0xffffffffu, t.n, from);
-                        t.len = __shfl_sync(0xffffffffu, t.len, from);
-    #pragma unroll
-                        for (int x = 0; x < kTlTiles; ++x) {
-                            const int first = t.j0 + x * tile_tokens, last = min(first + tile_tokens, t.n) - 1;
-                            const int end = first >= t.n || t.len < 0 ? 0 : a.causal ? t.len - t.n + 1 + last : t.len;
-                            t.blocks[x] = (max(end, 0) + kTlBlock - 1) / kTlBlock;
-                        }
-                        break;
-                    }
-                    t.i = -1;
-                }
-                if (k >= kTlItems) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&sh->item_empty[k % kTlItems], (k / kTlItems - 1) & 1));
+                tl_next(a, row_blocks, tile_tokens, at, t);
+                at = t.after;
+                if (k >= kTlItems) ok = attend_wait(a, &sh->item_empty[k % kTlItems], (k / kTlItems - 1) & 1);
                 if (ok && lane == 0) {
                     sh->item[k % kTlItems] = t;
                     ptx::mbar_arrive(&sh->item_full[k % kTlItems]);
@@ -402,7 +412,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     #pragma unroll
                 for (int x = 0; x < kTlTiles; ++x) {
                     if (!ok || t.blocks[x] == 0) continue;
-                    if (uses[x] > 0) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&sh->q_empty[x], (uses[x] - 1) & 1));
+                    if (uses[x] > 0) ok = attend_wait(a, &sh->q_empty[x], (uses[x] - 1) & 1);
                     if (ok && lane == 0) {
                         ptx::mbar_arrive_expect_tx(&sh->q_full[x], (uint32_t)(S::kSlabs * tile_tokens * a.group * 128));
                         for (int b = 0; b < S::kSlabs; ++b)
@@ -425,7 +435,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             bool ok = true;
             uint32_t n = 0, copy = 0;                    // blocks, slots so far
     #pragma unroll 1
-            for (uint32_t item = 0; ok && (ok = tl_take(sh, item, t)) && t.i >= 0; ++item) {
+            for (uint32_t item = 0; ok && (ok = tl_take(a, sh, item, t)) && t.i >= 0; ++item) {
                 const int most = max(t.blocks[0], t.blocks[1]);
     #pragma unroll 1
                 for (int j = 0; ok && j < most; ++j, ++n) {
@@ -447,8 +457,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     #pragma unroll 1
                     for (int v = 0; ok && v < 2; ++v, ++copy) {
                         const uint32_t slot = copy % S::kSlots, turn = copy / S::kSlots;
-                        if (turn > 0) ok = ptx::mbar_wait(&sh->code_empty[slot], (turn - 1) & 1);
-                        ok = __all_sync(0xffffffffu, ok);
+                        if (turn > 0) ok = attend_wait(a, &sh->code_empty[slot], (turn - 1) & 1);
                         if (!ok) break;
                         if (lane == 0) ptx::mbar_arrive_expect_tx(&sh->code_full[slot], bytes);
                         __syncwarp();
@@ -471,11 +480,12 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             // descriptors differ from these by multiples of 16 bytes in the address (their low 14 bits, which never carry)
             const uint64_t d_q = ptx::smem_desc_sw128(s_u32 + x * S::kOperand, 16, 1024), d_k = ptx::smem_desc_sw128(k_u32, 16, 1024);
             const uint64_t d_v = ptx::smem_desc_sw128(v_u32, S::kSlab, 1024);
+            auto wait = [&](uint64_t *bar, uint32_t parity) { return ptx::mbar_wait(bar, parity, a.polls); };
             bool ok = true;
             uint32_t n = 0, step = 0, items = 0, turns = 0;      // blocks and steps; this tile's items and blocks so far
             TlItem t;
     #pragma unroll 1
-            for (uint32_t item = 0; ok && (ok = tl_take(sh, item, t)) && t.i >= 0; ++item) {
+            for (uint32_t item = 0; ok && (ok = tl_take(a, sh, item, t)) && t.i >= 0; ++item) {
                 const int most = max(t.blocks[0], t.blocks[1]), mine = x ? t.blocks[1] : t.blocks[0];
                 // step j: products of block j - 1, scores of block j; n is block j's number.  A block that this tile sees nothing of is passed on
                 // once it is there (not before: its buffer's turns would be mixed up)
@@ -484,16 +494,17 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                     const uint32_t s = n & 1, s_before = s ^ 1;
                     const bool products = j > 0 && j <= mine, scores = j < mine;
                     // what is there early is waited for first, the weights last: their way to the next scores is the kernel's longest
-                    if (j > 0) ok = ptx::mbar_wait(&sh->v_full[s_before], ((n - 1) >> 1) & 1);
-                    if (j < most) ok = ok && ptx::mbar_wait(&sh->k_full[s], (n >> 1) & 1);
-                    if (j == 0 && mine > 0) ok = ok && ptx::mbar_wait(&sh->q_full[x], items & 1);
-                    if (j == 1 && mine > 0 && items > 0) ok = ok && ptx::mbar_wait(&sh->o_empty[x], (items - 1) & 1);   // (the last item's output is out of TMEM)
+                    if (j > 0) ok = wait(&sh->v_full[s_before], ((n - 1) >> 1) & 1);
+                    if (j < most) ok = ok && wait(&sh->k_full[s], (n >> 1) & 1);
+                    if (j == 0 && mine > 0) ok = ok && wait(&sh->q_full[x], items & 1);
+                    if (j == 1 && mine > 0 && items > 0) ok = ok && wait(&sh->o_empty[x], (items - 1) & 1);   // (the last item's output is out of TMEM)
                     // the other tile's turn before this
-                    if (x > 0 || step > 0) ok = ok && ptx::mbar_wait(&sh->turn[x ^ 1], (x ? step : step - 1) & 1);
+                    if (x > 0 || step > 0) ok = ok && wait(&sh->turn[x ^ 1], (x ? step : step - 1) & 1);
                     if (products) {
-                        ok = ok && ptx::mbar_wait(&sh->p_full[x], turns & 1);
+                        ok = ok && wait(&sh->p_full[x], turns & 1);
                         ++turns;
                     }
+                    ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     ptx::tc_fence_after();
                     if (products && issuer) {
@@ -541,15 +552,15 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         bool ok = true;
         uint32_t n = 0, copy = 0;
 #pragma unroll 1
-        for (uint32_t item = 0; ok && (ok = tl_take(sh, item, t)) && t.i >= 0; ++item) {
+        for (uint32_t item = 0; ok && (ok = tl_take(a, sh, item, t)) && t.i >= 0; ++item) {
             const int most = max(t.blocks[0], t.blocks[1]);
 #pragma unroll 1
             for (int j = 0; ok && j < 2 * most; ++j, ++copy) {
                 const bool values = j & 1;           // keys of a block, then its values
                 const uint32_t slot = copy % S::kSlots, s = n & 1;
-                ok = ptx::mbar_wait(&sh->code_full[slot], copy / S::kSlots & 1);
-                if (!ok) break;
-                if (n >= 2) ok = ptx::mbar_wait(values ? &sh->v_empty[s] : &sh->k_empty[s], ((n >> 1) - 1) & 1);
+                ok = ptx::mbar_wait(&sh->code_full[slot], copy / S::kSlots & 1, a.polls);
+                if (ok && n >= 2) ok = ptx::mbar_wait(values ? &sh->v_empty[s] : &sh->k_empty[s], ((n >> 1) - 1) & 1, a.polls);
+                ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 const uint32_t from = code_u32 + slot * S::kSlot + (32 * w + r) * D, to = (values ? v_u32 : k_u32) + s * S::kOperand + (32 * w + r) * 128;
                 if (values) tile_codes<D, true>(from, to, r, pc, low);
@@ -573,6 +584,11 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         int mine = -1, end = 0, blocks = 0, most = 0;
         const float factor = fabsf(a.scale_log2);    // (a negative scale is in the keys: the largest sum is the largest score)
         bool has = false, bad = false;
+        // the row's place among (row, query head) of the item, -1: it is none of the request's
+        auto place = [&](const TlItem &t) {
+            const int j_row = t.j0 + x * tile_tokens + jj;
+            return jj < tile_tokens && j_row < t.n ? (t.row0 + j_row) * a.q_heads + t.head * a.group + r_head : -1;
+        };
 #pragma unroll 1
         for (uint32_t item = 0;; ++item) {
             float top = kAtNothing, ref = kAtNothing, l = 0.f;   // m', r (what l is relative to: m' until a block is wide)
@@ -580,7 +596,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             const int warp_most = __shfl_sync(0xffffffffu, end, 31), warp_end = __shfl_sync(0xffffffffu, end, 0);   // (the first row sees the fewest tokens)
 #pragma unroll 1
             for (int j = 0; ok && j < blocks; ++j, ++turns) {
-                if (!(ok = ptx::mbar_wait(&sh->s_full[x], turns & 1))) break;
+                if (!(ok = attend_wait(a, &sh->s_full[x], turns & 1))) break;
                 ptx::tc_fence_after();
                 const float4 *group = sh->group[(n + j) % kTlGroupRing];
                 const int left = end - j * kTlBlock; // tokens of the block that the row sees
@@ -654,26 +670,18 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             }
             n += most;
             TlItem next;
-            if (!tl_take(sh, item, next)) {
-                ok = false;
-                sh->gave_up = 1;
-                next.i = -1;
-            }
+            next.i = -1;
+            if (ok) ok = tl_take(a, sh, item, next);
             int mine_next = -1, end_next = 0;
-            if (next.i >= 0) {
-                const int j_row = next.j0 + x * tile_tokens + jj;
-                if (jj < tile_tokens && j_row < next.n) mine_next = (next.row0 + j_row) * a.q_heads + next.head * a.group + r_head;
-                end_next = a.causal ? next.len - next.n + 1 + min(j_row, next.n - 1) : next.len;
+            if (ok && next.i >= 0) {
+                mine_next = place(next);
+                end_next = a.causal ? next.len - next.n + 1 + min(next.j0 + x * tile_tokens + jj, next.n - 1) : next.len;
             }
             const int blocks_next = next.i < 0 ? 0 : x ? next.blocks[1] : next.blocks[0];
             // ---- out
-            if (has) {
+            if (ok && has) {
                 const bool any = blocks > 0;
-                if (any && ok) {
-                    ok = ptx::mbar_wait(&sh->o_full[x], items & 1);
-                    ++items;
-                }
-                if (!ok) sh->gave_up = 1;
+                if (any) ok = attend_wait(a, &sh->o_full[x], items++ & 1);
                 ptx::tc_fence_after();
                 const bool nan = bad || sh->gave_up;
                 const float half = half_gap(top, ref), k = nan ? __uint_as_float(0x7fc00000u) : l == 0.f ? 0.f : 1.f / l * half;
@@ -700,6 +708,20 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                 }
                 if (mine >= 0 && a.lse) a.lse[mine] = nan ? k : l == 0.f ? -INFINITY : (ref + log2f(l)) * kAtLn2;
             }
+            if (!ok) {
+                // a wait gave up: the rows of this item and of all that the CTA would have taken behind it
+                sh->gave_up = 1;
+                int after = has ? sh->after[warp] : 0;
+                for (next.i = 0; next.i >= 0; mine = next.i < 0 ? -1 : place(next)) {
+                    if (mine >= 0) {
+                        for (int e = 0; e < D; ++e) a.out[(int64_t)mine * D + e] = __float2bfloat16(__uint_as_float(0x7fc00000u));
+                        if (a.lse) a.lse[mine] = __uint_as_float(0x7fc00000u);
+                    }
+                    tl_next(a, row_blocks, tile_tokens, after, next);
+                    after = next.after;
+                }
+                break;
+            }
             if (next.i < 0) break;
             has = true;
             bad = next.len < 0;
@@ -707,6 +729,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             end = end_next;
             blocks = blocks_next;
             most = max(next.blocks[0], next.blocks[1]);
+            sh->after[warp] = next.after;            // (kept for a wait that gives up alone)
         }
         ptx::tc_fence_before();
     }

@@ -262,3 +262,28 @@ def test_page_map_again_after_too_short_a_row():
     once = binding.PageMap.allocate(45, 2, DEV)
     binding.map_pages(off, one, free, _i32([0]), once, page_size=16, context_lens=ctx)
     assert torch.equal(wide, one) and all(torch.equal(a, b) for a, b in zip(m, once)) and m.state.tolist() == [3, 0]
+
+
+# ---- attention: waits that give up -------------------------------------------------------------------------------------
+
+@pytest.mark.usefixtures("bounds")
+@pytest.mark.parametrize("new,lens,qh,kh,dim,page", [
+    ([1], [500], 2, 2, 128, 64), ([1], [9000], 4, 1, 64, 128), ([1] * 70, [37 * i % 401 for i in range(70)], 12, 4, 64, 32),
+    ([3, 0, 5], [700, 9, 40], 8, 2, 128, 16), ([300, 0, 77], [2000, 0, 100], 3, 1, 64, 64), ([260] * 40, [300 + i for i in range(40)], 8, 8, 128, 64)])
+def test_attend_waits_that_give_up_leave_nan_and_no_trace(new, lens, qh, kh, dim, page, monkeypatch):
+    q, off, L, tables, cache = _batch(new, lens, qh, kh, dim, page, 3)
+    n = int(off[-1])
+
+    def call():
+        out, lse = torch.full_like(q, 3.0), torch.full(q.shape[:2], 3.0, device=DEV)
+        binding.cache_attend(q, off, L, tables, cache, max_q_len=max(new), max_seq_len=max(lens), out=out, lse=lse)
+        return out, lse
+
+    clean = call()
+    lib = binding.lib()
+    with monkeypatch.context() as m:
+        m.setattr(lib, "rtprune_cache_attend", lib.rtprune_test_cache_attend_expired)
+        for t in call():
+            assert t[:n].isnan().all() and (t[n:] == 3).all()
+    for a, b in zip(call(), clean):
+        assert torch.equal(a, b) and not a.isnan().any()
