@@ -287,3 +287,70 @@ def test_attend_waits_that_give_up_leave_nan_and_no_trace(new, lens, qh, kh, dim
             assert t[:n].isnan().all() and (t[n:] == 3).all()
     for a, b in zip(call(), clean):
         assert torch.equal(a, b) and not a.isnan().any()
+
+
+# ---- sizes of a serving batch ----------------------------------------------------------------------------------------
+
+def _check(q, off, L, tables, cache, max_q, max_len, rows):
+    """Some of the requests against the formulas, one by one."""
+    lse = torch.zeros(q.shape[:2], device=DEV)
+    out = binding.cache_attend(q, off, L, tables, cache, max_q_len=max_q, max_seq_len=max_len, lse=lse)
+    host = [t.cpu() for t in cache]
+    for i in rows:
+        a, b = int(off[i]), int(off[i + 1])
+        want, wlse, weight, dots, least = ref.attend(q[a:b].cpu(), [0, b - a], [int(L[i])], tables[i:i + 1].cpu(), host, q.shape[2] ** -0.5, True)
+        err = (2.0 ** -17 * dots)[..., None]
+        bound = 2.0 ** -8 * want.abs() + (2.0 ** -10 + 2 * err) * weight + 2.0 ** -25 * least + 1e-30
+        assert ((out[a:b].cpu().double() - want).abs() <= bound).all(), i
+        off_lse = (lse[a:b].cpu().double() - wlse).abs()
+        assert ((off_lse <= err[..., 0] + 2.0 ** -20 * (1 + wlse.abs())) | torch.isneginf(wlse)).all(), i
+
+
+@pytest.mark.usefixtures("bounds")
+@pytest.mark.parametrize("batch", [161, 256, 700, 4001])
+def test_attend_more_requests_than_threads_of_a_block(batch):
+    # a token of each, of lengths from nothing to several blocks, some requests without a row
+    new, lens = [int(i % 11 != 3) for i in range(batch)], [(i * 53) % 390 for i in range(batch)]
+    q, off, L, tables, cache = _batch(new, lens, 8, 2, 64, 16, batch)
+    _check(q, off, L, tables, cache, 1, 390, list(range(0, batch, 37)) + [batch - 1])
+
+
+@pytest.mark.usefixtures("bounds")
+def test_attend_more_requests_than_threads_of_several_rows():
+    new, lens = [(i * 7) % 5 for i in range(500)], [20 + (i * 29) % 900 for i in range(500)]
+    q, off, L, tables, cache = _batch(new, lens, 4, 4, 128, 64, 9)
+    _check(q, off, L, tables, cache, 4, 920, range(0, 500, 23))
+
+
+@pytest.mark.usefixtures("bounds")
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_attend_a_context_of_100000_tokens(new):
+    q, off, L, tables, cache = _batch([new, 1], [100003, 60], 8, 1, 128, 128, 4)
+    _check(q, off, L, tables, cache, new, 100003, [0, 1])
+
+
+@pytest.mark.usefixtures("bounds")
+@pytest.mark.parametrize("new,lens", [([1, 1], [100, 90]), ([6, 1], [100, 37]), ([90, 100], [100, 203])])
+def test_attend_reads_nothing_behind_a_length(new, lens):
+    """Codes behind a request's last token, in its last page, and the codes and scales of pages that are nobody's: whatever they are."""
+    q, off, L, tables, cache = _batch(new, lens, 2, 2, 64, 16, 4)
+    n = sum(new)
+
+    def call():
+        lse = torch.zeros(q.shape[:2], device=DEV)
+        return binding.cache_attend(q, off, L, tables, cache, max_q_len=max(new), max_seq_len=max(lens), lse=lse)[:n], lse[:n]
+
+    clean = call()
+    used = torch.zeros(cache.k.shape[0], dtype=torch.bool, device=DEV)
+    for i, length in enumerate(lens):
+        used[tables[i, :-(-length // 16)].long()] = True
+        last = tables[i, (length - 1) // 16].long()
+        for codes in (cache.k, cache.v):
+            codes[last, :, (length - 1) % 16 + 1:] = 127 if i else -127
+    assert not used.all()
+    for codes in (cache.k, cache.v):
+        codes[~used] = 127
+    for scale in (cache.k_scale, cache.v_scale):
+        scale[~used] = math.nan
+    for a, b in zip(call(), clean):
+        assert torch.equal(a, b)
