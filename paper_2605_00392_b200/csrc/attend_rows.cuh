@@ -747,8 +747,10 @@ attend_join_kernel(const __grid_constant__ AttendArgs a, const float *part, cons
     const float4 ml0 = part_ml[at0], ml1 = part_ml[at1];
     const float4 x0 = *reinterpret_cast<const float4 *>(part + at0 * D + col), x1 = *reinterpret_cast<const float4 *>(part + at1 * D + col);
     if (what.w == 0 || r >= (int)((uint32_t)what.z >> 26)) return;
+    // (nothing that the workspace says leads out of it, or below out of the outputs, whoever else should write there meanwhile)
+    const int parts = min(what.w, (int)(gridDim.x - blockIdx.x));
     float top = fmaxf(ml0.x, ml1.x), ref = fmaxf(ml0.z, ml1.z);
-    for (int p = 2; p < what.w; ++p) {
+    for (int p = 2; p < parts; ++p) {
         const float4 ml = part_ml[(int64_t)(2 * (blockIdx.x + p)) * kArRows + r];
         top = fmaxf(top, ml.x);
         ref = fmaxf(ref, ml.z);
@@ -756,7 +758,7 @@ attend_join_kernel(const __grid_constant__ AttendArgs a, const float *part, cons
     const float k0 = ex2(ml0.x - top), k1 = ex2(ml1.x - top);
     float4 o = make_float4(fmaf(x1.x, k1, x0.x * k0), fmaf(x1.y, k1, x0.y * k0), fmaf(x1.z, k1, x0.z * k0), fmaf(x1.w, k1, x0.w * k0));
     float l = fmaf(ml1.y, ex2(ml1.z - ref), ml0.y * ex2(ml0.z - ref));
-    for (int p = 2; p < what.w; ++p) {
+    for (int p = 2; p < parts; ++p) {
         const int64_t at = (int64_t)(2 * (blockIdx.x + p)) * kArRows + r;
         const float4 ml = part_ml[at];
         const float4 x = *reinterpret_cast<const float4 *>(part + at * D + col);
@@ -768,6 +770,7 @@ attend_join_kernel(const __grid_constant__ AttendArgs a, const float *part, cons
         o.w = fmaf(x.w, k, o.w);
     }
     const int m = (what.z & 0x3ffffff) + r, j = m / a.group;
+    if (what.x < 0 || what.x >= a.rows - j || (uint32_t)what.y >= (uint32_t)a.c.kv_heads) return;
     const int64_t row = (int64_t)(what.x + j) * a.q_heads + what.y * a.group + (m - j * a.group);
     const float half = half_gap(top, ref), k = l == 0.f ? 0.f : 1.f / l * half;
     uint2 w;
