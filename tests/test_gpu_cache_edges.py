@@ -354,3 +354,14 @@ def test_attend_reads_nothing_behind_a_length(new, lens):
         scale[~used] = math.nan
     for a, b in zip(call(), clean):
         assert torch.equal(a, b)
+
+
+@pytest.mark.usefixtures("bounds")
+@pytest.mark.parametrize("low,high", [(-60, 20), (-60, -50), (10, 20), (-61, 21)])
+@pytest.mark.parametrize("new,lens,causal", [([1, 3], [700, 65], True), ([150], [400], True), ([40, 9], [40, 9], True), ([150, 20], [300, 77], False)])
+def test_attend_scales_about_the_border_of_one_reference(new, lens, causal, low, high):
+    # no zeros: what has m' as the reference of its sum, through blocks seen in part
+    q, off, L, tables, cache = _batch(new, lens, 4, 2, 64, 16, 23)
+    cache.v_scale.copy_(torch.exp2(torch.randint(low, high + 1, cache.v_scale.shape, generator=torch.Generator().manual_seed(1)).float()))
+    for x in (q, 8 * q):
+        _check_tight(x, off, L, tables, cache, max(new), max(lens), causal)
