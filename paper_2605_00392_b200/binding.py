@@ -399,13 +399,16 @@ _CODE = {torch.bfloat16: BF16, torch.float32: FP32}
 _I32, _F32, _F64, _BF, _I8 = torch.int32, torch.float32, torch.float64, torch.bfloat16, torch.int8
 
 # These calls are a few microseconds each, of which the checks below are a good part: shapes and strides are taken once, devices
-# compared by number.
+# compared by number.  torch's own quick ways to the current device and stream are taken where it has them: its public ones make a Stream
+# object for every call.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 def _on_device(dev: int, stream: Optional[torch.cuda.Stream], where: str, call, *args) -> None:
     """call(stream handle, *args) with device number `dev` current."""
-    if dev == torch._C._cuda_getDevice():
-        status = call(torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream, *args)
+    if dev == _current_device():
+        status = call(_current_stream(dev) if stream is None else stream.cuda_stream, *args)
     else:
         with torch.cuda.device(dev):
             status = call(_stream_handle(stream), *args)

@@ -1,8 +1,8 @@
 """The operators behind the pruning where what lies beside a call's data could reach its results: other rows of a tile, other requests,
 shared memory of the kernel before."""
+import importlib.util
 import math
 
-import numpy as np
 import pytest
 import torch
 
@@ -365,3 +365,20 @@ def test_attend_scales_about_the_border_of_one_reference(new, lens, causal, low,
     cache.v_scale.copy_(torch.exp2(torch.randint(low, high + 1, cache.v_scale.shape, generator=torch.Generator().manual_seed(1)).float()))
     for x in (q, 8 * q):
         _check_tight(x, off, L, tables, cache, max(new), max(lens), causal)
+
+
+def test_calls_without_the_quick_ways_to_device_and_stream(monkeypatch):
+    # a torch that has not got them
+    with monkeypatch.context() as m:
+        for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
+            m.delattr(torch._C, name)
+        spec = importlib.util.find_spec(binding.__name__)
+        plain = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(plain)
+    assert plain._current_device is torch.cuda.current_device and binding._current_device is not torch.cuda.current_device
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        assert plain._current_stream(0) == binding._current_stream(0) == side.cuda_stream
+    q, off, L, tables, cache = _batch([2], [40], 2, 2, 64, 16, 1)
+    a, b = (x.cache_attend(q, off, L, tables, cache, max_q_len=2, max_seq_len=40) for x in (plain, binding))
+    assert torch.equal(a, b)
