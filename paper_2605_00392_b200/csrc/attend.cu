@@ -13,10 +13,10 @@ constexpr int kAtFewRows = 32, kAtFewTiles = 296;
 
 // Whether attend_rows_kernel takes the call: few rows of a kv head, so few tiles of 16 rows in the whole call that it has them all in one
 // go, two to an SM, where attend_tiles_kernel's of 256 rows leave most SMs without any, or more heads of a kv head than a tile has rows.
-// Rows against tiles, heads of 128, in us.  64 requests behind 1000 tokens, 10 heads: of 16 rows 52 / 108, 32 rows 93 / 112, 48 rows
-// 133 / 113, 128 rows 348 / 123; 16 requests behind 16000, 8 heads of 4: 32 rows 242 / 256, 64 rows 472 / 258.  Few tiles, 10 heads:
-// 220 (one image of 337 tokens) 10.7 / 13.2, 440 (two) 19.0 / 13.1, 320 (8 x 64 rows behind 1000) 31 / 29, 160 (2 x 128 behind 4000)
-// 47 / 82, 80 (128 behind 16000) 81 / 246.
+// Rows against tiles, heads of 128, in us.  64 requests behind 1000 tokens, 10 heads: of 16 rows 54 / 97, 32 rows 95 / 97, 48 rows
+// 132 / 98, 128 rows 329 / 108; 16 requests behind 16000, 8 heads of 4: 32 rows 257 / 234, 64 rows 500 / 239.  Few tiles, 10 heads:
+// 220 (one image of 337 tokens) 11.1 / 13.2, 440 (two) 19.6 / 12.8, 320 (8 x 64 rows behind 1000) 33 / 26, 160 (2 x 128 behind 4000)
+// 50 / 70, 80 (128 behind 16000) 85 / 236.
 static bool few_rows(int64_t batch, int64_t max_q_len, int64_t kv_heads, int group)
 {
     const int64_t rows = max_q_len * group;
@@ -84,8 +84,8 @@ static cudaError_t launch_rows(const AttendArgs &a, uint8_t *ws, cudaStream_t st
     if (!ctas) return cudaErrorInvalidDevice;
     const RowsLayout w = rows_layout(ctas, D);
     // every tile a CTA of its own, and a second kernel saved, where there are CTAs enough for as many as there can be and the longest is short.
-    // 10 heads, one token for one request of 256 tokens 6.9 us against 8.3 cut and joined, for one of 500 10.1 against 9.0 on the GPU but 18.8
-    // against 24.2 a call from the host, for 44 of 101 to 500 13.0 against 16.6; for one of 1001 16.7 against 10.4.
+    // 10 heads, one token for one request of 256 tokens 7.2 us against 8.7 cut and joined, for one of 500 10.8 against 9.1 on the GPU but 13.8
+    // against 16.1 a call from the host, for 44 of 101 to 500 13.6 against 16.9; for one of 1001 17.9 against 10.2.
     const int64_t tiles = (int64_t)a.batch * a.c.kv_heads * (((int64_t)std::min(a.max_q_len, a.rows) * a.group + R - 1) / R);
     const bool whole = tiles <= ctas && a.max_len <= kArWhole * kArBlock;
     static std::atomic<unsigned long long> ready{0};             // devices that know the kernel's shared memory
@@ -170,8 +170,8 @@ static rtprune_status_t cache_attend(void *cuda_stream, const void *q, int64_t q
         if (!expired) a.polls = ptx::kSpinLimit + 512u * (uint32_t)batch;
         uint8_t *ws = (uint8_t *)workspace;
         cudaStream_t st = (cudaStream_t)cuda_stream;
-        // tiles of 8 rows where a request has no more: 64 steps 37 us against 51 with 16, 16 long ones of 4 heads 116 against 153 (at 32 rows of
-        // a kv head, 16 requests behind 16000 tokens, 344 against 242)
+        // tiles of 8 rows where a request has no more: 64 steps 37 us against 52 with 16, 16 long ones of 4 heads 120 against 162 (at 32 rows of
+        // a kv head, 16 requests behind 16000 tokens, 360 against 257)
         const bool eight = (int64_t)max_q_len * a.group <= 8;
         const cudaError_t e = c.dim == 128 ? eight ? launch_rows<128, 8>(a, ws, st) : launch_rows<128, 16>(a, ws, st)
                                            : eight ? launch_rows<64, 8>(a, ws, st) : launch_rows<64, 16>(a, ws, st);

@@ -17,13 +17,15 @@
 // Everything large comes by bulk copies: with 227 KB of shared memory there are some 20 KB of L1 left, and ordinary loads of
 // 64 KB of queries, which need a line of it each while they are on their way, took 10,000 cycles.
 // A row's sums are rescaled only where 16 of its weights add up to more than 2^12 by the maximum so far: no weight has then left fp16's
-// range, and the sums, which are needed anyway, show it with less work than a maximum (772 us against 805 for 37 requests of 512 rows
-// that see 8512 tokens).  A tile's rows behind the request's last (the next request's queries, or whatever shared memory held where a
-// token's heads do not divide 128) are computed like the others, but have no voice in how a warp goes on: a row's bits do not hang on them.
+// range, and the sums, which are needed anyway, show it with less work than a maximum (4 % of the time of 37 requests of 512 rows that
+// see 8512 tokens).  Blocks seen in part, and an item's blocks from the first whose scales want a reference of their own for l, are gone
+// through with more care, in two passes.  A tile's rows behind the request's last (the next request's queries, or whatever shared
+// memory held where a token's heads do not divide 128) are computed like the others, but have no voice in how a warp goes on: a
+// row's bits do not hang on them.
 // Every wait is bounded, and the lanes of a warp take its result together.  Where one gives up its warp leaves; those that wait for it give
 // up too, and the softmax's warps write NaN to the rows of the item in work and of all that the CTA would have taken behind it.
 // Bound by the tensor cores and, about as much, by the exponentials: 128 x 128 scores take 1024 cycles of either (16 exponentials a
-// cycle and SM; two products of 128^3 at 4096 multiply-adds).  It takes 2200: 1.07 PFLOP/s at 512 rows over 8512 tokens, 211 us for 8 causal
+// cycle and SM; two products of 128^3 at 4096 multiply-adds).  It takes 2250: 1.05 PFLOP/s at 512 rows over 8512 tokens, 218 us for 8 causal
 // requests of 2783 tokens and 97 us for 64 of 300 to 375, 10 heads.  Keys that need no conversion would make that 15 % less, a softmax
 // without arithmetic as much: both want the issue slots and the shared memory that the products read at its full rate.
 #pragma once

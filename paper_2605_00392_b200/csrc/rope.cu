@@ -15,7 +15,7 @@ namespace rtp {
 // once, shared out over the lanes, while the first heads are on their way.  Angles in 64 bits, taken modulo a turn before they are rounded to
 // 32: at position 10^6 an fp32 angle would be off by 0.03.  Everything else in fp32, rounded once, at the store.
 // Each element is read and written once.  4999 rows of 40 heads in fp32: 41 us, 5.0 TB/s.  21568 rows of 20 heads in bf16: 54 us, 4.1 TB/s
-// (57 with a CTA for every four rows); there it is latency and issue slots (55 % of them) more than HBM: without the norm it takes 47, without
+// (57 with a CTA for every four rows); there it is latency and issue slots (58 % of them) more than HBM: without the norm it takes 47, without
 // the turning or the angles 53.  Other numbers of heads in flight and CTAs to an SM (5 at 4, 1 at 7) are as fast, and slower in fp32 (47, 53);
 // packed fp32 arithmetic is slower (64).
 constexpr int kRpWarps = 4;
