@@ -166,11 +166,11 @@ static rtprune_status_t cache_attend(void *cuda_stream, const void *q, int64_t q
         // a tile's first row has 26 bits of a word, and a CTA's blocks (of half a 148th of the line, and fewer) an int
         const int64_t most = std::min<int64_t>(max_q_len, rows) * a.group, tiles = (most + 7) / 8 * batch * c.kv_heads;
         if (most >= 1 << 26 || tiles * (max_seq_len / kArBlock + 1) / 64 > INT32_MAX) return RTPRUNE_ERR_UNSUPPORTED;
-        // a wait lasts as long as the fetching warp looks for the next request that has rows, at most
-        if (!expired) a.polls = ptx::kSpinLimit + 512u * (uint32_t)batch;
+        // a wait lasts as long as the fetching warp looks for the next request that has rows, at most (a thousand cycles for 32 of them)
+        if (!expired) a.polls = ptx::kSpinLimit + 32u * (uint32_t)batch;
         uint8_t *ws = (uint8_t *)workspace;
         cudaStream_t st = (cudaStream_t)cuda_stream;
-        // tiles of 8 rows where a request has no more: 64 steps 37 us against 52 with 16, 16 long ones of 4 heads 120 against 162 (at 32 rows of
+        // tiles of 8 rows where a request has no more: 64 steps 37 us against 52 with 16, 16 long ones of 4 heads 122 against 162 (at 32 rows of
         // a kv head, 16 requests behind 16000 tokens, 360 against 257)
         const bool eight = (int64_t)max_q_len * a.group <= 8;
         const cudaError_t e = c.dim == 128 ? eight ? launch_rows<128, 8>(a, ws, st) : launch_rows<128, 16>(a, ws, st)

@@ -20,7 +20,8 @@
 // The ring runs across tiles: the next one's codes are on their way while this one's warps are added up.
 // Steps with tokens that a row does not see, and all behind one whose scales want a reference of their own for l, take the largest s and s'
 // anew; the others only where a weight would pass 2^8.
-// 16 requests of 8000 to 32000 tokens, 32 heads on 8: 120 us, 5.4 TB/s; 64 of 350 to 1500, 10 heads: 37 us, 4.1 TB/s.
+// 16 requests of 8000 to 32000 tokens, 32 heads on 8: 122 us, 5.3 TB/s; 64 of 350 to 1500, 10 heads: 38 us, 4.1 TB/s
+// (of 4096 in a batch of which the others have no rows 49 us).
 #pragma once
 #include "attend.cuh"
 
@@ -62,7 +63,8 @@ struct ArPlace {
             blocks = max(1, (len + kArBlock - 1) / kArBlock);
         }
     }
-    // `steps` blocks on, within the tile or to the next one's first (the line ends before the batch does: the caller counts)
+    // `steps` blocks on, within the tile or to the next one's first, for a whole warp (the line ends before the batch does: the caller
+    // counts, and does not ask for what is behind the line's end).  Requests without rows are passed over 32 at a time.
     template <int R> __device__ void next(const AttendArgs &a, int steps)
     {
         block += steps;
@@ -71,8 +73,21 @@ struct ArPlace {
         if (++tile < tiles) return;
         tile = 0;
         if (++head < a.c.kv_heads) return;
-        do request<R>(a, i + 1);
-        while (tiles == 0 && i < a.batch);
+        head = tiles = 0;
+        uint32_t found = 0;
+        for (++i; i < a.batch; i += 32) {
+            const int mine = i + (int)(threadIdx.x & 31);
+            found = __ballot_sync(0xffffffffu, mine < a.batch && attend_request(a, mine, row0, n, len));
+            if (found) break;
+        }
+        if (!found) return;
+        const int from = __ffs(found) - 1;
+        i += from;
+        row0 = __shfl_sync(0xffffffffu, row0, from);
+        n = __shfl_sync(0xffffffffu, n, from);
+        len = __shfl_sync(0xffffffffu, len, from);
+        tiles = (n * a.group + R - 1) / R;
+        blocks = max(1, (len + kArBlock - 1) / kArBlock);
     }
 };
 
@@ -231,7 +246,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
                 const int page = t < at.len ? attend_page(a, at.i, t) : -1;
                 next_block = page < 0 ? -1 : page * a.c.kv_heads + at.head;
                 next_slot = t & (a.c.page_size - 1);
-                at.next<R>(a, 1);
+                if (look + 1 < todo) at.next<R>(a, 1);
             }
             if (look > 0) {
                 const uint32_t s = n % S::kStages, turn = n / S::kStages, to = ring + s * 2 * S::kBytes;
@@ -729,7 +744,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a, int whole_tiles, float 
                                                    1 + (rest + chunk - 1) / chunk)
                                        : make_int4(0, 0, 0, 0);
         }
-        at.next<R>(a, steps);
+        if (left > 0) at.next<R>(a, steps);
     }
 }
 

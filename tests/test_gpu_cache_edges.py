@@ -382,3 +382,34 @@ def test_calls_without_the_quick_ways_to_device_and_stream(monkeypatch):
     q, off, L, tables, cache = _batch([2], [40], 2, 2, 64, 16, 1)
     a, b = (x.cache_attend(q, off, L, tables, cache, max_q_len=2, max_seq_len=40) for x in (plain, binding))
     assert torch.equal(a, b)
+
+
+# ---- attention: batches padded with requests that have no rows --------------------------------------------------------------
+
+@pytest.mark.usefixtures("bounds")
+@pytest.mark.parametrize("batch", [40, 256, 4097, 65535])
+@pytest.mark.parametrize("where", ["behind", "ahead", "between", "spread"])
+def test_attend_padded_batches(batch, where):
+    real = [(1, 700), (3, 64), (1, 1), (2, 900), (1, 0), (4, 300), (1, 129), (1, 517)]
+    at = {"behind": range(8), "ahead": range(batch - 8, batch), "between": [0, 1, 2, 3, batch - 4, batch - 3, batch - 2, batch - 1],
+          "spread": range(0, batch // 8 * 8, batch // 8)}[where]
+    new, lens = [0] * batch, [0] * batch
+    for i, (n, length) in zip(at, real):
+        new[i], lens[i] = n, length
+    q, off, L, tables, cache = _batch([n for n, _ in real], [x for _, x in real], 6, 2, 128, 64, 3)
+    padded = torch.full((batch, tables.shape[1]), -1, dtype=torch.int32, device=DEV)
+    padded[list(at)] = tables
+    got = []
+    for o, lengths, t in ((off, L, tables), (_i32([0] + torch.tensor(new).cumsum(0).tolist()), _i32(lens), padded)):
+        lse = torch.full(q.shape[:2], 3.0, device=DEV)
+        out = binding.cache_attend(q, o, lengths, t, cache, max_q_len=4, max_seq_len=900, out=torch.full_like(q, 3.0), lse=lse)
+        got.append((out, lse))
+    want, wlse, weight, dots, least = ref.attend(q.cpu(), off.tolist(), L.tolist(), tables.cpu(), [t.cpu() for t in cache], 128 ** -0.5, True)
+    n = int(off[-1])
+    err = (2.0 ** -17 * dots[:n])[..., None]
+    bound = 2.0 ** -8 * want[:n].abs() + (2.0 ** -10 + 2 * err) * weight[:n] + 2.0 ** -25 * least[:n] + 1e-30
+    empty = torch.isinf(wlse[:n])
+    for out, lse in got:
+        assert ((out[:n].cpu().double() - want[:n]).abs() <= bound).all() and (out[n:] == 3).all()
+        assert torch.equal(torch.isneginf(lse[:n].cpu()), empty) and (lse[n:] == 3).all()
+        assert ((lse[:n].cpu().double() - wlse[:n])[~empty].abs() <= err[..., 0][~empty] + 2.0 ** -20 * (1 + wlse[:n][~empty].abs())).all()
