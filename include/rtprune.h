@@ -435,12 +435,12 @@ rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *q, int64_t 
                                       const rtprune_cache_t *cache, float scale, int32_t causal, void *out, float *lse,
                                       void *workspace, size_t workspace_bytes);
 
-/* Test aid: rtprune_cache_attend with waits that give up at once (NaN in every row of a request). */
+/* Test aid: rtprune_cache_attend with waits that give up after `polls` looks (0: at once, NaN in every row of a request). */
 rtprune_status_t rtprune_test_cache_attend_expired(void *cuda_stream, const void *q, int64_t q_stride, int64_t rows, int32_t q_heads,
                                                    const int32_t *offsets, const int32_t *seq_lens, int32_t batch, int32_t max_q_len,
                                                    int64_t max_seq_len, const int32_t *block_tables, int64_t table_stride, int32_t max_pages,
                                                    const rtprune_cache_t *cache, float scale, int32_t causal, void *out, float *lse,
-                                                   void *workspace, size_t workspace_bytes);
+                                                   void *workspace, size_t workspace_bytes, int32_t polls);
 
 /*
  * Test aid: makes the library's bounded device-side waits run out without any fault.  Launches one small

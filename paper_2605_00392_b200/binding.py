@@ -93,7 +93,7 @@ def lib() -> ctypes.CDLL:
     L.rtprune_cache_write.argtypes = [vp, i32, vp, i64, vp, i64, i64, vp, pc]
     L.rtprune_cache_attend_workspace.argtypes = [i32, i32, i64, i32, i32, i32, ctypes.POINTER(sz)]
     L.rtprune_cache_attend.argtypes = [vp, vp, i64, i64, i32, vp, vp, i32, i32, i64, vp, i64, i32, pc, f32, i32, vp, vp, vp, sz]
-    L.rtprune_test_cache_attend_expired.argtypes = L.rtprune_cache_attend.argtypes
+    L.rtprune_test_cache_attend_expired.argtypes = L.rtprune_cache_attend.argtypes + [i32]
     L.rtprune_profile_enable.argtypes = [vp, i32]
     L.rtprune_profile_read.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(ctypes.c_float),
                                        ctypes.POINTER(ctypes.c_char_p)]

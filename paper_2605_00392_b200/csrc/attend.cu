@@ -135,11 +135,11 @@ extern "C" rtprune_status_t rtprune_cache_attend_workspace(int32_t batch, int32_
 
 namespace rtp {
 
-// rtprune_cache_attend; expired: waits that give up at once.
+// rtprune_cache_attend; polls: after which its waits give up, -1: as many as the call's sizes ask.
 static rtprune_status_t cache_attend(void *cuda_stream, const void *q, int64_t q_stride, int64_t rows, int32_t q_heads, const int32_t *offsets,
                                      const int32_t *seq_lens, int32_t batch, int32_t max_q_len, int64_t max_seq_len,
                                      const int32_t *block_tables, int64_t table_stride, int32_t max_pages, const rtprune_cache_t *cache,
-                                     float scale, int32_t causal, void *out, float *lse, void *workspace, size_t workspace_bytes, bool expired)
+                                     float scale, int32_t causal, void *out, float *lse, void *workspace, size_t workspace_bytes, int32_t polls)
 {
     CacheView c;
     rtprune_status_t status;
@@ -167,7 +167,7 @@ static rtprune_status_t cache_attend(void *cuda_stream, const void *q, int64_t q
         const int64_t most = std::min<int64_t>(max_q_len, rows) * a.group, tiles = (most + 7) / 8 * batch * c.kv_heads;
         if (most >= 1 << 26 || tiles * (max_seq_len / kArBlock + 1) / 64 > INT32_MAX) return RTPRUNE_ERR_UNSUPPORTED;
         // a wait lasts as long as the fetching warp looks for the next request that has rows, at most (a thousand cycles for 32 of them)
-        if (!expired) a.polls = ptx::kSpinLimit + 32u * (uint32_t)batch;
+        a.polls = polls >= 0 ? (uint32_t)polls : ptx::kSpinLimit + 32u * (uint32_t)batch;
         uint8_t *ws = (uint8_t *)workspace;
         cudaStream_t st = (cudaStream_t)cuda_stream;
         // tiles of 8 rows where a request has no more: 64 steps 37 us against 52 with 16, 16 long ones of 4 heads 122 against 162 (at 32 rows of
@@ -181,7 +181,8 @@ static rtprune_status_t cache_attend(void *cuda_stream, const void *q, int64_t q
     if (tile_row_blocks(a) * batch * c.kv_heads > INT32_MAX / 2) return RTPRUNE_ERR_UNSUPPORTED;
     // waits last as long as the items that are ahead, at most (five of them, some 7000 cycles a block each), and the search for the next one (a
     // thousand cycles for 32 numbers); a poll is 20 cycles or more
-    if (!expired)
+    a.polls = (uint32_t)polls;
+    if (polls < 0)
         a.polls = ptx::kSpinLimit + 4096u * (uint32_t)std::min<int64_t>(max_seq_len / kTlBlock + 1, 1 << 19) +
                   16u * (uint32_t)(tile_row_blocks(a) * batch * c.kv_heads / std::max(device_sms(), 1) + 1);
     const cudaError_t e = c.dim == 128 ? launch_tiles<128>(a, (cudaStream_t)cuda_stream) : launch_tiles<64>(a, (cudaStream_t)cuda_stream);
@@ -199,7 +200,7 @@ extern "C" rtprune_status_t rtprune_cache_attend(void *cuda_stream, const void *
                                                  void *out, float *lse, void *workspace, size_t workspace_bytes)
 {
     return rtp::cache_attend(cuda_stream, q, q_stride, rows, q_heads, offsets, seq_lens, batch, max_q_len, max_seq_len, block_tables, table_stride,
-                             max_pages, cache, scale, causal, out, lse, workspace, workspace_bytes, false);
+                             max_pages, cache, scale, causal, out, lse, workspace, workspace_bytes, -1);
 }
 
 extern "C" rtprune_status_t rtprune_test_cache_attend_expired(void *cuda_stream, const void *q, int64_t q_stride, int64_t rows, int32_t q_heads,
@@ -207,8 +208,8 @@ extern "C" rtprune_status_t rtprune_test_cache_attend_expired(void *cuda_stream,
                                                               int32_t max_q_len, int64_t max_seq_len, const int32_t *block_tables,
                                                               int64_t table_stride, int32_t max_pages, const rtprune_cache_t *cache,
                                                               float scale, int32_t causal, void *out, float *lse, void *workspace,
-                                                              size_t workspace_bytes)
+                                                              size_t workspace_bytes, int32_t polls)
 {
     return rtp::cache_attend(cuda_stream, q, q_stride, rows, q_heads, offsets, seq_lens, batch, max_q_len, max_seq_len, block_tables, table_stride,
-                             max_pages, cache, scale, causal, out, lse, workspace, workspace_bytes, true);
+                             max_pages, cache, scale, causal, out, lse, workspace, workspace_bytes, std::max(polls, 0));
 }

@@ -282,9 +282,15 @@ def test_attend_waits_that_give_up_leave_nan_and_no_trace(new, lens, qh, kh, dim
     clean = call()
     lib = binding.lib()
     with monkeypatch.context() as m:
-        m.setattr(lib, "rtprune_cache_attend", lib.rtprune_test_cache_attend_expired)
-        for t in call():
-            assert t[:n].isnan().all() and (t[n:] == 3).all()
+        m.setattr(lib, "rtprune_cache_attend", lambda *args: lib.rtprune_test_cache_attend_expired(*args, polls))
+        for polls in (0, 1, 1, 2, 2, 3, 5):
+            out, lse = call()
+            gone = out[:n].isnan().all(-1)
+            # a row is there, bit for bit, or gone
+            assert polls > 0 or gone.all()
+            assert torch.equal(gone, out[:n].isnan().any(-1)) and torch.equal(gone, lse[:n].isnan())
+            assert torch.equal(out[:n][~gone], clean[0][:n][~gone]) and torch.equal(lse[:n][~gone], clean[1][:n][~gone])
+            assert (out[n:] == 3).all() and (lse[n:] == 3).all()
     for a, b in zip(call(), clean):
         assert torch.equal(a, b) and not a.isnan().any()
 
